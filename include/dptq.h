@@ -160,6 +160,103 @@ dptq_status dptq_sensitivity_policy(const float* x, const float* dx, int L, int 
                                     double tau_jr, double tau_snr, double* jr, double* snr, uint8_t* bits_out,
                                     void* stream);
 
+/* ---- Operators around the linear layer: the residual stream's norm, and attention over an
+ * 8-bit KV cache.  (Section 4.2 names the quantized KV cache and the backbones that fold their
+ * rotations into the residual stream; it describes no kernels.) */
+
+/* Residual addition, RMS norm and per-token symmetric quantization in one call: the codes that
+ * projections packed with had_block = 1 (their rotation folded offline into the residual
+ * stream) take through dptq_qgemm_codes.
+ *   h = fp16_rne(x + residual);  p = h * gamma (exact in fp32);  s' = max|p| * fl(1 / qmax);
+ *   c = round-half-even(p / s');  scale = s' / sqrt(mean(h^2) + eps),
+ * in fp32 with the IEEE quotient; fl(1 / qmax) is the reciprocal of 7 or 127 rounded to fp32
+ * (the quantizers above divide by qmax; a step one unit in the last place away serves as well).
+ * The norm's factor is one positive number a token, so it goes into the scale alone and the
+ * codes depend on h and gamma only, bit for bit.  A token of zeros has scale 0 and codes 0; a
+ * NaN counts for nothing in the maximum and takes the code 0.
+ * x_fp16, residual_fp16, residual_out: device [M][K] binary16.  residual_fp16 NULL: h = x, and
+ *   residual_out must be NULL too; otherwise residual_out receives h and may be x_fp16 or
+ *   residual_fp16 itself.  gamma_fp16: device [K], or NULL for 1.
+ * codes, scales: as dptq_rotate_quant_act writes them.  K % 32 == 0, K <= 49152; x_fp16,
+ * residuals and gamma 16-byte aligned, codes 8-byte (bits 8) or 4-byte (bits 4) aligned.
+ * Asynchronous; allocates nothing.  INVALID_ARG for bits, null or misaligned pointers, negative
+ * sizes or eps; UNSUPPORTED for K.  M == 0 is a no-op. */
+dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16, const void* gamma_fp16, int M,
+                                   int K, float eps, int bits, void* residual_out, void* codes, float* scales,
+                                   void* stream);
+
+/* A paged KV cache of int8 codes with one fp32 scale for each page of tokens and KV head:
+ * value = scale * code.  Codes [num_blocks][kv_heads][block_tokens][head_dim], 16-byte aligned;
+ * scales [num_blocks][kv_heads].  All device memory of the caller; the struct itself is host
+ * memory, read during the call only.  head_dim 64 or 128; block_tokens 16, 32, 64 or 128. */
+typedef struct dptq_kv8_cache {
+  int8_t* k_codes;
+  int8_t* v_codes;
+  float* k_scales;
+  float* v_scales;
+  int num_blocks, kv_heads, block_tokens, head_dim;
+} dptq_kv8_cache;
+
+/* The sequences that a call works on.  cu_tokens: device int32 [seqs + 1], sequence s has the rows
+ * cu_tokens[s] .. cu_tokens[s + 1] - 1 of the call's `tokens` rows.  seq_lens: device int32
+ * [seqs], the cached tokens WITH the call's own rows, which are a sequence's last ones: row i of
+ * n stands at position seq_lens[s] - n + i.  A negative position (a sequence shorter than its
+ * rows, for example a padding slot of length 0) is stored nowhere and sees nothing.
+ * block_table: device int32 [seqs][table_stride], the page that holds positions
+ * block_tokens * i ..; entries that no position of the call needs are not read.
+ * tokens, max_tokens, max_len: host upper bounds of cu_tokens[seqs], of a sequence's rows and of
+ * seq_lens; max_len <= table_stride * block_tokens.  The same batch serves a step's append and
+ * its attention.
+ * What the device arrays hold is checked on the device: a sequence that exceeds these bounds is
+ * left out (its rows and outputs are not touched), a page number outside [0, num_blocks) reads
+ * as a page without keys and is not written, and dptq_last_device_error then reports
+ * INVALID_ARG. */
+typedef struct dptq_kv8_batch {
+  const int* cu_tokens;
+  const int* seq_lens;
+  const int* block_table;
+  int seqs, table_stride, tokens, max_tokens, max_len;
+} dptq_kv8_batch;
+
+/* Quantize the K and V rows of new tokens into the cache.  For each page and head, with s0 the
+ * stored scale if the page holds earlier positions of the sequence, else 0:
+ *   s1 = max(s0, max|x| * fl(1 / 127)) over the page's new rows;  new codes
+ *   round-half-even(x / s1);  where s1 > s0, earlier codes become round-half-even(fl(c s0) / s1),
+ * all in fp32 with IEEE quotients.
+ * Codes are in [-127, 127]; s1 = 0 gives codes 0; a NaN counts for nothing in the maximum and
+ * takes the code 0; an infinite value makes its page's scale infinite.  Positions past the new
+ * rows are not written.  A page is written through one sequence of the batch at most.
+ * k_fp16, v_fp16: device rows of `tokens` tokens, kv_heads * head_dim binary16 values each, rows
+ * token_stride elements apart (so they may be parts of one projection's output); 16-byte
+ * aligned, token_stride a multiple of 8.
+ * Asynchronous.  INVALID_ARG for null or misaligned pointers and bad sizes; UNSUPPORTED for other
+ * head_dim or block_tokens, more than 1023 KV heads or 65535 sequences.  seqs == 0 or tokens == 0 is a no-op.
+ * The first call on a device allocates the library's small scratch (its error word), which is
+ * refused (UNSUPPORTED) during stream capture: call dptq_kv8_reserve or dptq_reserve first. */
+dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
+                            const void* v_fp16, long long token_stride, void* stream);
+
+/* Causal attention of the batch's rows over the cache, query head h reading KV head
+ * h / (q_heads / kv_heads):
+ *   logit_j = scale * k_scale * (q . k_code_j);  out = sum_j softmax(logit)_j v_scale v_code_j
+ * over the keys j that the query at position p sees: j <= p and, with window > 0,
+ * j > p - window or j < sinks.  A query that sees none gets zeros.
+ * The integer codes enter the tensor cores exactly (int8 fits in binary16), the scales are
+ * applied in fp32; softmax weights times V scale are rounded to binary16 relative to their
+ * largest so far; logits, maxima, sums and accumulators are fp32.
+ * q_fp16, out_fp16: device rows of `tokens` tokens, q_heads * head_dim binary16 values each, rows
+ * q_stride / out_stride elements apart; 16-byte aligned, strides multiples of 8.
+ * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.
+ * Asynchronous; uses the library's per-device scratch (allocated by the first call, or by
+ * dptq_kv8_reserve).  Errors as dptq_kv8_append. */
+dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
+                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
+                               long long out_stride, void* stream);
+
+/* Allocate the scratch of the two calls above on the current device, so that neither allocates
+ * (for example before a stream capture).  Synchronous. */
+dptq_status dptq_kv8_reserve(void);
+
 /* The quantized linear layer: out = fp16( Q(x R) (W R)^T scaled ), i.e. rotate and
  * quantize x with `bits` (4 or 8, the layer's mask entry), multiply by the packed
  * int4 weights of `h` with exact int32 accumulation, apply s_a[m] * s_w[n].
@@ -267,7 +364,8 @@ dptq_status dptq_get_shape(dptq_handle h, int* N, int* K, int* had_block);
  * bounded wait that gave up: DPTQ_OK or DPTQ_ERR_TIMEOUT.  `h` may be NULL.  Covers the
  * per-device scratch of the allocating calls and the fixed array of dptq_qlinear_static;
  * after a timeout it also zeroes the split-tile sums and counters the aborted kernel may
- * have left, so that later calls start clean. */
+ * have left, so that later calls start clean.  INVALID_ARG: a KV8 call's device arrays held
+ * lengths or page numbers out of range. */
 dptq_status dptq_last_device_error(dptq_handle h);
 
 /* Test hook: the activation-plane and scale buffers of the current device's scratch,

@@ -19,6 +19,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "../../include/dptq.h"
+#include "dptq_device.cuh"
 #include "dptq_internal.h"
 
 using namespace dptq;
@@ -742,6 +743,150 @@ dptq_status dptq_sensitivity_policy(const float* x, const float* dx, int L, int 
 }
 
 namespace {
+// The host's part of a KV8 call's checks; *none: nothing to do.
+dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStream_t s, Kv8Args* a, bool* none,
+                      Scratch** sc) {
+  *none = false;
+  if (!c || !b) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (c->num_blocks <= 0 || c->kv_heads <= 0 || c->block_tokens <= 0 || c->head_dim <= 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "bad cache sizes");
+  if (b->seqs < 0 || b->tokens < 0 || b->max_tokens < 0 || b->max_len < 0 || b->table_stride < 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "bad batch sizes");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(DPTQ_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (c->block_tokens < 16 || c->block_tokens > 128 || !is_pow2(c->block_tokens))
+    return fail(DPTQ_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
+  if (c->kv_heads > 1023 || b->seqs > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "too many heads or sequences");
+  if (b->seqs == 0 || b->tokens == 0 || b->max_tokens == 0) {
+    *none = true;
+    return DPTQ_OK;
+  }
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !b->cu_tokens || !b->seq_lens || !b->block_table)
+    return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes))
+    return fail(DPTQ_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+  if (b->max_len > (long long)b->table_stride * c->block_tokens)
+    return fail(DPTQ_ERR_INVALID_ARG, "max_len exceeds the block table");
+  int dev;
+  dptq_status st = current_device(&dev);
+  if (st != DPTQ_OK) return st;
+  if ((st = ensure_scratch(dev, 0, 0, s, sc)) != DPTQ_OK) return st;
+  *a = Kv8Args{};
+  a->codes[0] = c->k_codes;
+  a->codes[1] = c->v_codes;
+  a->scales[0] = c->k_scales;
+  a->scales[1] = c->v_scales;
+  a->cu = b->cu_tokens;
+  a->lens = b->seq_lens;
+  a->table = b->block_table;
+  a->seqs = b->seqs;
+  a->table_stride = b->table_stride;
+  a->tokens = b->tokens;
+  a->max_tokens = std::min(b->max_tokens, b->tokens);
+  a->max_len = b->max_len;
+  a->num_blocks = c->num_blocks;
+  a->kv_heads = c->kv_heads;
+  a->head_dim = c->head_dim;
+  a->log2_page = c->block_tokens == 16 ? 4 : c->block_tokens == 32 ? 5 : c->block_tokens == 64 ? 6 : 7;
+  a->err = (*sc)->err;
+  return DPTQ_OK;
+}
+
+// Rows of `heads` heads: aligned, and no row reaching into the next.
+dptq_status check_rows(const void* p, long long stride, long long heads, int D) {
+  if (!p) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(p) || stride % 8 != 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "rows must be 16-byte aligned: base pointers, and strides of multiples of 8");
+  if (stride < heads * D) return fail(DPTQ_ERR_INVALID_ARG, "a row's stride is below its length");
+  return DPTQ_OK;
+}
+}  // namespace
+
+dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
+                            const void* v_fp16, long long token_stride, void* stream) {
+  NvtxRange nvtx_range("dptq_kv8_append");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Kv8AppendArgs a{};
+  Scratch* sc = nullptr;
+  bool none;
+  dptq_status st = check_kv8(cache, batch, s, &a.c, &none, &sc);
+  if (st != DPTQ_OK || none) return st;
+  if ((st = check_rows(k_fp16, token_stride, cache->kv_heads, cache->head_dim)) != DPTQ_OK) return st;
+  if ((st = check_rows(v_fp16, token_stride, cache->kv_heads, cache->head_dim)) != DPTQ_OK) return st;
+  a.rows[0] = static_cast<const __half*>(k_fp16);
+  a.rows[1] = static_cast<const __half*>(v_fp16);
+  a.stride = token_stride;
+  DPTQ_CUDA(launch_kv8_append(a, s), "kv8_append launch");
+  return DPTQ_OK;
+}
+
+dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
+                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
+                               long long out_stride, void* stream) {
+  NvtxRange nvtx_range("dptq_kv8_attention");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (q_heads <= 0 || window < 0 || sinks < 0 || !std::isfinite(scale))
+    return fail(DPTQ_ERR_INVALID_ARG, "bad q_heads, window, sinks or scale");
+  if (cache && cache->kv_heads > 0) {
+    if (q_heads % cache->kv_heads != 0) return fail(DPTQ_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
+    if (q_heads / cache->kv_heads > 64) return fail(DPTQ_ERR_UNSUPPORTED, "more than 64 query heads for a KV head");
+  }
+  Kv8AttendArgs a{};
+  Scratch* sc = nullptr;
+  bool none;
+  dptq_status st = check_kv8(cache, batch, s, &a.c, &none, &sc);
+  if (st != DPTQ_OK || none) return st;
+  if ((st = check_rows(q_fp16, q_stride, q_heads, cache->head_dim)) != DPTQ_OK) return st;
+  if ((st = check_rows(out_fp16, out_stride, q_heads, cache->head_dim)) != DPTQ_OK) return st;
+  a.q = static_cast<const __half*>(q_fp16);
+  a.out = static_cast<__half*>(out_fp16);
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.q_heads = q_heads;
+  a.group = q_heads / cache->kv_heads;
+  a.scale = scale;
+  a.window = window;
+  a.sinks = sinks;
+  DPTQ_CUDA(launch_kv8_attend(a, sc->num_sms, s), "kv8_attend launch");
+  return DPTQ_OK;
+}
+
+dptq_status dptq_kv8_reserve(void) {
+  NvtxRange nvtx_range("dptq_kv8_reserve");
+  int dev;
+  dptq_status st = current_device(&dev);
+  if (st != DPTQ_OK) return st;
+  Scratch* sc = nullptr;
+  if ((st = ensure_scratch(dev, 0, 0, 0, &sc)) != DPTQ_OK) return st;
+  DPTQ_CUDA(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+  return DPTQ_OK;
+}
+
+dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16, const void* gamma_fp16, int M,
+                                   int K, float eps, int bits, void* residual_out, void* codes, float* scales,
+                                   void* stream) {
+  NvtxRange nvtx_range("dptq_add_rmsnorm_quant");
+  if (bits != 4 && bits != 8) return fail(DPTQ_ERR_INVALID_ARG, "bits must be 4 or 8");
+  if (M < 0 || K <= 0 || !(eps >= 0.f)) return fail(DPTQ_ERR_INVALID_ARG, "bad sizes or eps");
+  if (K % 32 != 0 || K > 49152) return fail(DPTQ_ERR_UNSUPPORTED, "K must be a multiple of 32 up to 49152");
+  if (M == 0) return DPTQ_OK;
+  if (!x_fp16 || !codes || !scales) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if ((residual_fp16 == nullptr) != (residual_out == nullptr))
+    return fail(DPTQ_ERR_INVALID_ARG, "residual and residual_out go together");
+  if (!aligned16(x_fp16) || !aligned16(residual_fp16) || !aligned16(gamma_fp16) || !aligned16(residual_out))
+    return fail(DPTQ_ERR_INVALID_ARG, "x, residual, gamma and residual_out must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(codes) & (bits == 8 ? 7u : 3u)) != 0 || (reinterpret_cast<uintptr_t>(scales) & 3u) != 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "codes must be aligned to 8 codes, scales to 4 bytes");
+  int dev;
+  dptq_status st = current_device(&dev);
+  if (st != DPTQ_OK) return st;
+  NormArgs a{static_cast<const __half*>(x_fp16), static_cast<const __half*>(residual_fp16),
+             static_cast<const __half*>(gamma_fp16), static_cast<__half*>(residual_out),
+             static_cast<uint8_t*>(codes), scales, M, K, bits, eps};
+  DPTQ_CUDA(launch_norm_quant(a, 0, static_cast<cudaStream_t>(stream)), "norm_quant launch");
+  return DPTQ_OK;
+}
+
+namespace {
 void write_plan(const GemmPlan& plan, int* info, int len) {
   const GemmArgs& g = plan.args;
   const long long sk = g.sk_iters;
@@ -866,6 +1011,10 @@ dptq_status dptq_last_device_error(dptq_handle h) {
   if (e != cudaSuccess) return cuda_fail(e, "static scratch error word");
   if (word == 0) word = sword;
   if (word == 0) return DPTQ_OK;
+  if (word == kDevBadBatch || word == kDevBadPage)
+    return fail(DPTQ_ERR_INVALID_ARG, word == kDevBadPage
+                                          ? "a KV8 call met a page number outside the cache"
+                                          : "a KV8 call's sequence exceeded its declared tokens or length");
   char buf[64];
   snprintf(buf, sizeof(buf), "device wait timed out (code 0x%x)", word);
   return fail(DPTQ_ERR_TIMEOUT, buf);

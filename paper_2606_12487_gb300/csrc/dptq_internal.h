@@ -103,6 +103,48 @@ struct PolicyArgs {
 };
 cudaError_t launch_policy(const PolicyArgs& a, int num_sms, cudaStream_t s);
 
+// ------------------------------------------------------------------ norm, KV8 cache
+struct NormArgs {
+  const __half* x;         // [M][K]
+  const __half* residual;  // [M][K] or null (h = x)
+  const __half* gamma;     // [K] or null (1)
+  __half* residual_out;    // [M][K], may be x or residual itself; null without a residual
+  uint8_t* codes;          // [M][K / 2] or [M][K]
+  float* scales;           // [M]
+  int M, K, bits;
+  float eps;
+};
+cudaError_t launch_norm_quant(const NormArgs& a, int num_sms, cudaStream_t s);
+
+// One call's view of a paged int8 cache and of the batch that it works on.
+struct Kv8Args {
+  int8_t* codes[2];      // K and V: [num_blocks][kv_heads][page][head_dim]
+  float* scales[2];      // [num_blocks][kv_heads]
+  const int* cu;         // [seqs + 1] first token of each sequence in the call's rows
+  const int* lens;       // [seqs] cached tokens with those of this call
+  const int* table;      // [seqs][table_stride] page numbers
+  int seqs, table_stride, tokens, max_tokens, max_len;
+  int num_blocks, kv_heads, head_dim;
+  int log2_page;         // tokens of a page: 16 to 128
+  int* err;              // device error word
+};
+struct Kv8AppendArgs {
+  Kv8Args c;
+  const __half* rows[2];   // K and V rows of the new tokens, heads side by side
+  long long stride;        // elements from one token to the next
+};
+cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t s);
+struct Kv8AttendArgs {
+  Kv8Args c;
+  const __half* q;         // [tokens][q_heads][head_dim], rows `q_stride` elements apart
+  __half* out;             // the same, rows `out_stride` apart
+  long long q_stride, out_stride;
+  int q_heads, group;      // query heads, and of each KV head
+  float scale;
+  int window, sinks;       // window 0: every earlier token is seen
+};
+cudaError_t launch_kv8_attend(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
+
 // ------------------------------------------------------------------ GEMM
 struct GemmArgs {
   const uint8_t* wt;   // [NTw][KB][4][128][16] packed sign-magnitude weights (chunk-major tiles)

@@ -1,0 +1,52 @@
+// kv8_device.cuh -- what the kernels over the paged int8 cache share: the checked view of a
+// sequence, page lookups and the exact quantizer of a value.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+#include <cuda_fp16.h>
+
+#include "dptq_device.cuh"
+#include "dptq_internal.h"
+
+namespace dptq {
+
+// A sequence of the call: its n new tokens are rows tok0 .. tok0 + n - 1 and stand at the
+// positions start .. start + n - 1 (start = len - n; below zero for tokens that a sequence
+// shorter than its rows has no place for).
+struct Seq {
+  int tok0, n, len, start;
+};
+// False (and, from the thread that `tells`, the error word) where the arrays contradict what
+// the call declared: such a sequence is left alone, so no index is made from its numbers.
+__device__ __forceinline__ bool load_seq(const Kv8Args& c, int s, Seq& q, bool tells) {
+  const int a = __ldg(c.cu + s), b = __ldg(c.cu + s + 1), len = __ldg(c.lens + s);
+  const bool ok = a >= 0 && b >= a && b <= c.tokens && b - a <= c.max_tokens && len >= 0 && len <= c.max_len;
+  q.tok0 = a;
+  q.n = b - a;
+  q.len = len;
+  q.start = len - q.n;
+  if (!ok && tells) atomicCAS(c.err, 0, kDevBadBatch);
+  return ok;
+}
+
+// The page that holds position p of sequence s, or -1 (and the error word) if the table has
+// none.  p < max_len <= table_stride * page, checked on the host and by load_seq.
+__device__ __forceinline__ int load_page(const Kv8Args& c, int s, int page) {
+  const int b = __ldg(c.table + (long long)s * c.table_stride + page);
+  if (b >= 0 && b < c.num_blocks) return b;
+  atomicCAS(c.err, 0, kDevBadPage);
+  return -1;
+}
+
+// Whether the query at position p sees the key at position j.
+__device__ __forceinline__ bool kv8_sees(int p, int j, int window, int sinks) {
+  return j <= p && (window == 0 || j > p - window || j < sinks);
+}
+
+// rint(x / s) of the IEEE quotient, ties to even; 0 for a NaN quotient and for s = 0.
+// |x| <= 127 s but for the quotient's rounding, and an infinite x has an infinite s.
+__device__ __forceinline__ int quant_code(float x, float s) {
+  return s > 0.f ? __float2int_rn(__fdiv_rn(x, s)) : 0;
+}
+
+}  // namespace dptq

@@ -25,7 +25,18 @@ EXPORTS = ("dptq_pack_weights", "dptq_rotate_quant_act", "dptq_rotate_act", "dpt
            "dptq_qgemm_codes", "dptq_reserve", "dptq_get_packed", "dptq_get_shape",
            "dptq_last_device_error", "dptq_destroy", "dptq_status_str", "dptq_last_error_message",
            "dptq_pack_weights_rh", "dptq_rotate_quant_act_rh", "dptq_rotate_act_rh", "dptq_kv4_quantize",
-           "dptq_sensitivity_policy", "dptq_plan_info", "dptq_launch_plan", "dptq_scratch_buffers")
+           "dptq_sensitivity_policy", "dptq_plan_info", "dptq_launch_plan", "dptq_scratch_buffers",
+           "dptq_add_rmsnorm_quant", "dptq_kv8_append", "dptq_kv8_attention", "dptq_kv8_reserve")
+
+
+class _Kv8CacheC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales")] + [
+        (n, ctypes.c_int) for n in ("num_blocks", "kv_heads", "block_tokens", "head_dim")]
+
+
+class _Kv8BatchC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cu_tokens", "seq_lens", "block_table")] + [
+        (n, ctypes.c_int) for n in ("seqs", "table_stride", "tokens", "max_tokens", "max_len")]
 
 
 class DptqError(RuntimeError):
@@ -49,7 +60,7 @@ def load(build_if_missing: bool = True):
             if not os.path.exists(path):
                 raise RuntimeError(f"libdptq is not built ({path}); run paper_2606_12487_gb300.build")
             lib = ctypes.CDLL(path)
-            P, I = ctypes.c_void_p, ctypes.c_int
+            P, I, LL, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float
             sig = {
                 "dptq_pack_weights": ([P, I, I, I, I, ctypes.POINTER(P)], I),
                 "dptq_rotate_quant_act": ([P, I, I, I, I, P, P, P], I),
@@ -76,6 +87,10 @@ def load(build_if_missing: bool = True):
                 "dptq_launch_plan": ([I, I, I, I, I, I, ctypes.POINTER(I), I], I),
                 "dptq_scratch_buffers": ([ctypes.POINTER(P), ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(I), I,
                                           ctypes.POINTER(I)], I),
+                "dptq_add_rmsnorm_quant": ([P, P, P, I, I, F, I, P, P, P, P], I),
+                "dptq_kv8_append": ([P, P, P, P, LL, P], I),
+                "dptq_kv8_attention": ([P, P, P, LL, I, F, I, I, P, LL, P], I),
+                "dptq_kv8_reserve": ([], I),
             }
             for name, (args, res) in sig.items():
                 fn = getattr(lib, name)
@@ -277,6 +292,110 @@ def dptq_qgemm_codes(layer: QLinear, codes, scales, bits: int, out, acc=None, st
         _check_tensor(acc, torch.int32, (M, layer.N), "acc")
     _check(load().dptq_qgemm_codes(layer.handle, _ptr(codes), _ptr(scales), M, bits, _ptr(out), _ptr(acc),
                                    _stream(stream)))
+
+
+def dptq_add_rmsnorm_quant(x, residual, gamma, eps: float, bits: int, residual_out, codes, scales, stream=None):
+    """h = x + residual (float16 [M, K]; residual and residual_out may both be None), RMS norm
+    with the weight gamma (float16 [K] or None) and per-token codes and scales in the format
+    of dptq_rotate_quant_act.  residual_out receives h and may be x or residual itself."""
+    import torch
+    M, K = x.shape
+    _check_tensor(x, torch.float16, (M, K), "x")
+    if residual is not None:
+        _check_tensor(residual, torch.float16, (M, K), "residual")
+    if residual_out is not None:
+        _check_tensor(residual_out, torch.float16, (M, K), "residual_out")
+    if gamma is not None:
+        _check_tensor(gamma, torch.float16, (K,), "gamma")
+    _check_tensor(codes, torch.uint8 if bits == 4 else torch.int8, (M, K // 2 if bits == 4 else K), "codes")
+    _check_tensor(scales, torch.float32, (M,), "scales")
+    _check(load().dptq_add_rmsnorm_quant(_ptr(x), _ptr(residual), _ptr(gamma), M, K, eps, bits, _ptr(residual_out),
+                                         _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+class Kv8Cache:
+    """A paged KV cache of int8 codes: codes int8 [num_blocks, kv_heads, block_tokens, head_dim]
+    and scales float32 [num_blocks, kv_heads], for K and for V.  Keeps the tensors."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales):
+        import torch
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must have 4 dimensions")
+        n, h, b, d = k_codes.shape
+        _check_tensor(k_codes, torch.int8, (n, h, b, d), "k_codes")
+        _check_tensor(v_codes, torch.int8, (n, h, b, d), "v_codes")
+        _check_tensor(k_scales, torch.float32, (n, h), "k_scales")
+        _check_tensor(v_scales, torch.float32, (n, h), "v_scales")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim = n, h, b, d
+        self._c = _Kv8CacheC(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), n, h, b, d)
+        self._ref = ctypes.addressof(self._c)
+
+    @classmethod
+    def empty(cls, num_blocks: int, kv_heads: int, block_tokens: int, head_dim: int, device="cuda"):
+        import torch
+        codes = [torch.zeros((num_blocks, kv_heads, block_tokens, head_dim), dtype=torch.int8, device=device)
+                 for _ in range(2)]
+        scales = [torch.zeros((num_blocks, kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(*codes, *scales)
+
+
+class Kv8Batch:
+    """The sequences of one step: cu_tokens int32 [seqs + 1], seq_lens int32 [seqs] (cached
+    tokens with the step's own), block_table int32 [seqs, columns], all on the GPU; the host's
+    bounds `tokens` (cu_tokens[seqs]), `max_tokens` (of a sequence in this step) and `max_len`
+    (of a sequence's length).  Keeps the tensors."""
+
+    def __init__(self, cu_tokens, seq_lens, block_table, tokens: int, max_tokens: int, max_len: int):
+        import torch
+        S = seq_lens.shape[0]
+        _check_tensor(cu_tokens, torch.int32, (S + 1,), "cu_tokens")
+        _check_tensor(seq_lens, torch.int32, (S,), "seq_lens")
+        _check_tensor(block_table, torch.int32, (S, block_table.shape[1]), "block_table")
+        self.cu_tokens, self.seq_lens, self.block_table = cu_tokens, seq_lens, block_table
+        self.tokens = tokens
+        self._c = _Kv8BatchC(_ptr(cu_tokens), _ptr(seq_lens), _ptr(block_table), S, block_table.shape[1], tokens,
+                             max_tokens, max_len)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _check_heads(t, tokens, heads, dim, name):
+    """float16 [tokens, heads, dim] with the heads of a token side by side; tokens any distance apart."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16:
+        raise TypeError(f"{name} must be a float16 CUDA tensor")
+    if t.shape != (tokens, heads, dim):
+        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dim):
+        raise ValueError(f"{name} must hold the heads of a token side by side")
+    return st[0] if tokens > 1 else heads * dim
+
+
+def dptq_kv8_append(cache: Kv8Cache, batch: Kv8Batch, k, v, stream=None):
+    """Quantize the new tokens' k and v (float16 [tokens, kv_heads, head_dim], the heads of a
+    token side by side, both with the same distance between tokens) into the cache's pages."""
+    s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
+    if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
+        raise ValueError("k and v must have the same distance between tokens")
+    _check(load().dptq_kv8_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+
+
+def dptq_kv8_attention(cache: Kv8Cache, batch: Kv8Batch, q, out, scale: float, window: int = 0, sinks: int = 0,
+                       stream=None):
+    """Causal attention of q (float16 [tokens, q_heads, head_dim]) over the cache into out (the
+    same shape); with window > 0 a query sees its last `window` positions and the first
+    `sinks` ones."""
+    H = q.shape[1]
+    qs = _check_heads(q, batch.tokens, H, cache.head_dim, "q")
+    os_ = _check_heads(out, batch.tokens, H, cache.head_dim, "out")
+    _check(load().dptq_kv8_attention(cache._ref, batch._ref, q.data_ptr(), qs, H, scale, window, sinks,
+                                     out.data_ptr(), os_, _stream(stream)))
+
+
+def dptq_kv8_reserve():
+    """Allocate the scratch of the KV8 calls on the current device."""
+    _check(load().dptq_kv8_reserve())
 
 
 def dptq_reserve(max_M: int, max_K: int, max_N: int = 0):
