@@ -176,6 +176,8 @@ struct Scratch {
   uint32_t* pmax = nullptr;
   int* err = nullptr;
   int num_sms = 0;
+  float* kv8_ws = nullptr;            // partial attention results and their arrival counters,
+  uint32_t* kv8_counters = nullptr;   // from the first attention call or dptq_kv8_reserve on
   std::vector<std::pair<void*, size_t>> retired;   // superseded act / sa buffers, still allocated
 };
 std::mutex g_mu;
@@ -273,6 +275,28 @@ dptq_status ensure_scratch(int dev, size_t act_bytes, size_t sa_count, cudaStrea
     sc.sa_count = count;
   }
   *out = &sc;
+  return DPTQ_OK;
+}
+
+// The attention's part of the scratch, of a size that the device alone fixes.
+dptq_status ensure_kv8_scratch(Scratch* sc, cudaStream_t s) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  if (sc->kv8_ws) return DPTQ_OK;
+  if (capturing(s)) return fail(DPTQ_ERR_UNSUPPORTED, "scratch must grow during stream capture: call dptq_kv8_reserve first");
+  float* ws = nullptr;
+  uint32_t* counters = nullptr;
+  const size_t words = sizeof(uint32_t) * kv8_counter_words(sc->num_sms);
+  cudaError_t e = dev_malloc(reinterpret_cast<void**>(&ws), kv8_ws_bytes(sc->num_sms));
+  if (e == cudaSuccess) e = dev_malloc(reinterpret_cast<void**>(&counters), words);
+  if (e == cudaSuccess) e = cudaMemset(counters, 0, words);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    if (ws) cudaFree(ws);
+    if (counters) cudaFree(counters);
+    return cuda_fail(e, "scratch allocation");
+  }
+  sc->kv8_ws = ws;
+  sc->kv8_counters = counters;
   return DPTQ_OK;
 }
 
@@ -846,7 +870,11 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   a.scale = scale;
   a.window = window;
   a.sinks = sinks;
-  DPTQ_CUDA(launch_kv8_attend(a, sc->num_sms, s), "kv8_attend launch");
+  if ((st = ensure_kv8_scratch(sc, s)) != DPTQ_OK) return st;
+  a.ws = sc->kv8_ws;
+  a.counters = sc->kv8_counters;
+  const bool decode = (long long)a.c.max_tokens * a.group <= kDecodeRows;
+  DPTQ_CUDA(decode ? launch_kv8_decode(a, sc->num_sms, s) : launch_kv8_attend(a, sc->num_sms, s), "kv8_attention launch");
   return DPTQ_OK;
 }
 
@@ -857,8 +885,7 @@ dptq_status dptq_kv8_reserve(void) {
   if (st != DPTQ_OK) return st;
   Scratch* sc = nullptr;
   if ((st = ensure_scratch(dev, 0, 0, 0, &sc)) != DPTQ_OK) return st;
-  DPTQ_CUDA(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
-  return DPTQ_OK;
+  return ensure_kv8_scratch(sc, 0);
 }
 
 dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16, const void* gamma_fp16, int M,

@@ -142,7 +142,19 @@ struct Kv8AttendArgs {
   int q_heads, group;      // query heads, and of each KV head
   float scale;
   int window, sinks;       // window 0: every earlier token is seen
+  float* ws;               // partial results of shared (sequence, head)s
+  uint32_t* counters;      // their arrivals (zero between launches)
 };
+constexpr int kDecodeRows = 16;   // most rows of a (sequence, KV head) in the decode kernel
+// Decode grids: CTAs an SM for up to 8 and up to 16 rows; each CTA leaves partial results of two
+// (sequence, head)s at most: weighted values, maximum and sum of each row.
+constexpr int kDecodeCtas8 = 3, kDecodeCtas16 = 2;
+inline size_t kv8_ws_bytes(int num_sms) {
+  const int r8 = kDecodeCtas8 * 8, r16 = kDecodeCtas16 * 16;
+  return (size_t)num_sms * 2 * (r8 > r16 ? r8 : r16) * (128 + 2) * sizeof(float);
+}
+inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * kDecodeCtas8; }
+cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_kv8_attend(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 
 // ------------------------------------------------------------------ GEMM
