@@ -153,7 +153,7 @@ inline size_t kv8_ws_bytes(int num_sms) {
   const int r8 = kDecodeCtas8 * 8, r16 = kDecodeCtas16 * 16;
   return (size_t)num_sms * 2 * (r8 > r16 ? r8 : r16) * (128 + 2) * sizeof(float);
 }
-inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * kDecodeCtas8; }
+inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * kDecodeCtas8 * 3; }
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_kv8_attend(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 

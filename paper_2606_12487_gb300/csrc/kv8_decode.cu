@@ -10,12 +10,15 @@
 // accumulators, joined through shared memory once per share.
 //
 // A warp multiplies with 16 x 8 x 16 register MMAs (rows of q x keys, then rows x dims): with
-// one row tile of at most 16 rows there is nothing for tcgen05's 128-row tiles to do, and the
-// fragments come straight from global memory into registers, without shared memory:
+// one row tile of at most 16 rows there is nothing for tcgen05's 128-row tiles to do.  Each
+// warp keeps its own ring of steps in shared memory, filled by asynchronous 16-byte copies
+// (no barrier between warps), and reads fragments in whatever order suits 16-byte reads:
 //   * logits: the B fragment of key g takes any order of the dims as long as q has the same,
-//     so a lane takes 16 consecutive bytes of its key's row, 64 bytes a quad and load;
+//     so a lane takes 16 consecutive bytes of its key's row at a time;
 //   * values: the B fragment of dim g takes any order of the dims across its tiles, so a lane
-//     takes D / 8 consecutive bytes of four keys, a whole row for eight lanes.
+//     takes D / 8 consecutive bytes of four keys.
+// Each 16-byte chunk of a 128-byte line stands at its place xor the line's number mod 8, so
+// that neither read meets a bank twice.
 // int8 -> binary16 is exact: a byte c + 128 under the exponent of 1024 is 1152 + c.
 //
 // Softmax in base 2 on x_j = log2(e) scale sk (q . ck_j) + log2(sv): the weights that go into
@@ -32,6 +35,8 @@ namespace dptq {
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 constexpr int kDecKeys = 32;        // keys of a step
 constexpr int kDecMinSteps = 16;    // fewest steps that a CTA is started for
+constexpr int kDecJoin = 12;        // most partial results joined at once
+constexpr int kDecJoinMost = 32;    // of a group, and groups: sqrt of a grid of 1024 CTAs at most
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
@@ -108,27 +113,39 @@ __device__ __forceinline__ int block_scan(int v, int* red, int& total) {   // ex
   return base + x - v;
 }
 
-// One step's loads of a warp.
+// A warp's ring: steps of 32 K rows, then 32 V rows, and what goes with a step.
 template <int D>
-struct StepRegs {
-  uint4 k[4][D / 64];       // [8-key tile][64-dim chunk]
-  uint4 v[2][4];            // [16-key group][key]  (D = 64: the low half)
-  float a[2], b[2], inv[2];   // per 16 keys: logit factor, log2(sv), 1 / sv
+struct alignas(128) Ring {
+  static constexpr int kStages = 256 / D;            // 16 KB a warp
+  static constexpr int kHalf = kDecKeys * D;         // bytes of K (and of V)
+  uint8_t kv[kStages][2 * kHalf];
+  float scale[kStages][4];                           // sk of the two 16-key groups, then sv
+  int blk[kStages][2];                               // their pages, -1: none
 };
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(on ? 4 : 0) : "memory");
+}
+// Where byte `at` (a multiple of 8) of a half of a step stands.
+__device__ __forceinline__ uint32_t swz(uint32_t at) { return at ^ (((at >> 7) & 7u) << 4); }
 
 template <int D, int RT>   // RT: 8-row halves of the row tile that hold rows (1 or 2)
 __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeCtas16) kv8_decode_kernel(const Kv8AttendArgs A) {
   constexpr int VB = D / 8;                       // bytes of a V row for one lane; n-tiles of the second product
   constexpr int R = 8 * RT, kSlot = R * D + 2 * R;   // floats of a partial result
-  extern __shared__ __align__(16) float sm[];     // [warps][R][D], then maxima and sums [warps][R] each
+  constexpr int NS = Ring<D>::kStages, H = Ring<D>::kHalf;
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ float s_m[kDecWarps][R], s_l[kDecWarps][R];
   __shared__ int red[kDecWarps], found[3];
+  __shared__ float j_m[kDecJoinMost][R], j_l[kDecJoinMost][R];
   __shared__ uint32_t arrived;
-  float* so = sm;
-  float* s_m = sm + kDecWarps * R * D;
-  float* s_l = s_m + kDecWarps * R;
+  Ring<D>* rings = reinterpret_cast<Ring<D>*>(sm);   // (each warp's becomes its weighted values [R][D] at a share's end)
   const Kv8Args& c = A.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int P = 1 << c.log2_page;
+  Ring<D>& ring = rings[warp];
 
   // ---- this CTA's share
   long long total = 0;
@@ -194,7 +211,7 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint2 v = make_uint2(0u, 0u);
-        if (row < rows) v = __ldg(reinterpret_cast<const uint2*>(src + (k >> 2) * 64 + 16 * t + 4 * (k & 3)));
+        if (row < rows) v = __ldg(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
         qf[k][r] = v.x;
         qf[k][RT + r] = v.y;
       }
@@ -221,69 +238,55 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
       for (int h = 0; h < 2; ++h)
         if (group_seen(key + 16 * h)) blk[h] = load_page(c, s, (key + 16 * h) >> c.log2_page);
     };
-    auto load_k = [&](int i, const int (&blk)[2], StepRegs<D>& x) {
-      const int in = key_of(i) & (P - 1);
+    // copies step i into its stage; always one group, so that the waits can count
+    auto issue = [&](int i, int stage, const int (&blk)[2]) {
+      if (i < i1) {
+        const int in = key_of(i) & (P - 1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const size_t hb = (size_t)(blk[h] < 0 ? 0 : blk[h]) * c.kv_heads + head;
-        const int r0 = (in + 16 * h) & (P - 1);
-        const int8_t* src = c.codes[0] + ((hb << c.log2_page) + r0 + g) * D + 16 * t;
-        x.a[h] = x.b[h] = x.inv[h] = 0.f;
-        if (blk[h] >= 0) {
-          x.a[h] = __ldg(c.scales[0] + hb);
-          x.b[h] = __ldg(c.scales[1] + hb);
-        }
+        for (int h = 0; h < 2; ++h) {
+          const bool on = blk[h] >= 0;
+          const size_t hb = (size_t)(on ? blk[h] : 0) * c.kv_heads + head;
+          const size_t row = ((hb << c.log2_page) + ((in + 16 * h) & (P - 1))) * D + 16 * lane;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-          for (int ch = 0; ch < D / 64; ++ch)
-            x.k[2 * h + u][ch] = blk[h] >= 0 ? __ldg(reinterpret_cast<const uint4*>(src + 8 * u * D + 64 * ch))
-                                             : make_uint4(0u, 0u, 0u, 0u);
-      }
-    };
-    auto load_v = [&](int i, const int (&blk)[2], StepRegs<D>& x) {
-      const int in = key_of(i) & (P - 1);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const size_t hb = (size_t)(blk[h] < 0 ? 0 : blk[h]) * c.kv_heads + head;
-        const int r0 = (in + 16 * h) & (P - 1);
-        const int8_t* src = c.codes[1] + ((hb << c.log2_page) + r0 + 2 * t) * D + VB * g;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int8_t* p = src + ((u >> 1) * 8 + (u & 1)) * D;
-          x.v[h][u] = make_uint4(0u, 0u, 0u, 0u);
-          if (blk[h] >= 0) {
-            if constexpr (D == 128) {
-              x.v[h][u] = __ldg(reinterpret_cast<const uint4*>(p));
-            } else {
-              const uint2 y = __ldg(reinterpret_cast<const uint2*>(p));
-              x.v[h][u].x = y.x;
-              x.v[h][u].y = y.y;
-            }
-          }
+            for (int u = 0; u < D / 32; ++u)
+              copy16(smem_u32(ring.kv[stage]) + kv * H + swz(16 * D * h + 512 * u + 16 * lane),
+                     c.codes[kv] + row + 512 * u, on);
+          if (lane < 2) copy4(smem_u32(&ring.scale[stage][2 * lane + h]), c.scales[lane] + hb, on);
+          if (lane == 0) ring.blk[stage][h] = blk[h];
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     };
 
-    StepRegs<D> x;
-    int blk[2], next[2];
-    int i = i0 + warp;
-    pages_of(i, blk);
-    if (i < i1) {
-      load_k(i, blk, x);
-      load_v(i, blk, x);
+    int blk[2], i = i0 + warp, stage = 0;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+      pages_of(i + k * kDecWarps, blk);
+      issue(i + k * kDecWarps, k, blk);
     }
     for (; i < i1; i += kDecWarps) {
-      pages_of(i + kDecWarps, next);
+      pages_of(i + NS * kDecWarps, blk);   // (used after this step)
+      asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
+      __syncwarp();
+      const uint8_t* sk = ring.kv[stage];
+      const uint8_t* sv = sk + H;
+      const bool held0 = ring.blk[stage][0] >= 0, held1 = ring.blk[stage][1] >= 0;
+      const float4 scl = *reinterpret_cast<const float4*>(ring.scale[stage]);
       const int key = key_of(i);
       float sc[4][4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+        uint4 kw[D / 64];
+#pragma unroll
+        for (int ch = 0; ch < D / 64; ++ch)
+          kw[ch] = *reinterpret_cast<const uint4*>(sk + swz((8 * n + g) * D + D / 4 * t + 16 * ch));
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint4& w4 = x.k[n][k >> 2];
+          const uint4& w4 = kw[k >> 2];
           const uint32_t w = (k & 3) == 0 ? w4.x : (k & 3) == 1 ? w4.y : (k & 3) == 2 ? w4.z : w4.w;
           uint32_t b0, b1;
           widen4(w, b0, b1);
@@ -297,13 +300,11 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
       float fa[2], fb[2], inv[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float sv = fmaxf(x.b[h], 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-        fa[h] = x.a[h] * (A.scale * 1.4426950408889634f);
-        fb[h] = __log2f(sv);
-        inv[h] = __frcp_rn(sv);
+        const float v = fmaxf(h ? scl.w : scl.z, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
+        fa[h] = (h ? scl.y : scl.x) * (A.scale * 1.4426950408889634f);
+        fb[h] = __log2f(v);
+        inv[h] = __frcp_rn(v);
       }
-      const bool held0 = blk[0] >= 0, held1 = blk[1] >= 0;
-      if (i + kDecWarps < i1) load_k(i + kDecWarps, next, x);
       float top[RT];
 #pragma unroll
       for (int r = 0; r < RT; ++r) top[r] = m[r];
@@ -356,44 +357,59 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
         }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
+{
+          uint32_t vw[4][VB / 4];
 #pragma unroll
-        for (int w = 0; w < VB / 4; ++w) {
-          uint32_t b0[4], b1[4];
-          auto word = [&](const uint4& v) { return w == 0 ? v.x : w == 1 ? v.y : w == 2 ? v.z : v.w; };
-          widen_pairs(word(x.v[h][0]), word(x.v[h][1]), b0);
-          widen_pairs(word(x.v[h][2]), word(x.v[h][3]), b1);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float (&acc)[2 * RT] = o[4 * w + e];
-            if constexpr (RT == 1) {
-              float d[4] = {acc[0], acc[1], 0.f, 0.f};
-              mma_16816(d, pf[h][0], 0u, pf[h][1], 0u, b0[e], b1[e]);
-              acc[0] = d[0];
-              acc[1] = d[1];
+          for (int u = 0; u < 4; ++u) {
+            const uint8_t* p = sv + swz((16 * h + 2 * t + (u >> 1) * 8 + (u & 1)) * D + VB * g);
+            if constexpr (D == 128) {
+              const uint4 v = *reinterpret_cast<const uint4*>(p);
+              vw[u][0] = v.x, vw[u][1] = v.y, vw[u][2] = v.z, vw[u][3] = v.w;
             } else {
-              mma_16816(acc, pf[h][0], pf[h][1], pf[h][2], pf[h][3], b0[e], b1[e]);
+              const uint2 v = *reinterpret_cast<const uint2*>(p);
+              vw[u][0] = v.x, vw[u][1] = v.y;
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < VB / 4; ++w) {
+            uint32_t b0[4], b1[4];
+            widen_pairs(vw[0][w], vw[1][w], b0);
+            widen_pairs(vw[2][w], vw[3][w], b1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float (&acc)[2 * RT] = o[4 * w + e];
+              if constexpr (RT == 1) {
+                float d[4] = {acc[0], acc[1], 0.f, 0.f};
+                mma_16816(d, pf[h][0], 0u, pf[h][1], 0u, b0[e], b1[e]);
+                acc[0] = d[0];
+                acc[1] = d[1];
+              } else {
+                mma_16816(acc, pf[h][0], pf[h][1], pf[h][2], pf[h][3], b0[e], b1[e]);
+              }
             }
           }
         }
-      if (i + kDecWarps < i1) load_v(i + kDecWarps, next, x);
-      blk[0] = next[0];
-      blk[1] = next[1];
+      __syncwarp();
+      issue(i + NS * kDecWarps, stage, blk);
+      stage = stage + 1 == NS ? 0 : stage + 1;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
 
     // ---- the CTA's warps joined
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-      float* dst = so + (warp * R + g + 8 * r) * D;
+      float* dst = reinterpret_cast<float*>(&ring) + (g + 8 * r) * D;
 #pragma unroll
       for (int j = 0; j < VB; ++j) {
         dst[2 * t * VB + j] = o[j][2 * r];
         dst[(2 * t + 1) * VB + j] = o[j][2 * r + 1];
       }
       if (t == 0) {
-        s_m[warp * R + g + 8 * r] = m[r];
-        s_l[warp * R + g + 8 * r] = l[r];
+        s_m[warp][g + 8 * r] = m[r];
+        s_l[warp][g + 8 * r] = l[r];
       }
     }
     __syncthreads();
@@ -404,13 +420,13 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
       const int row = k / D, d = k - row * D;
       float M = -INFINITY, L = 0.f, O = 0.f;
 #pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) M = fmaxf(M, s_m[w * R + row]);
+      for (int w = 0; w < kDecWarps; ++w) M = fmaxf(M, s_m[w][row]);
       const float mm = M == -INFINITY ? 0.f : M;
 #pragma unroll
       for (int w = 0; w < kDecWarps; ++w) {
-        const float f = exp2_fast(s_m[w * R + row] - mm);
-        L = fmaf(f, s_l[w * R + row], L);
-        O = fmaf(f, so[(w * R + row) * D + d], O);
+        const float f = exp2_fast(s_m[w][row] - mm);
+        L = fmaf(f, s_l[w][row], L);
+        O = fmaf(f, reinterpret_cast<const float*>(&rings[w])[k], O);
       }
       if (whole) {
         const int tok = row / A.group, hh = row - tok * A.group;
@@ -427,30 +443,76 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
     if (!whole) {
       // CTA b holds steps b total / ctas ..: the one that holds step i is ((i + 1) ctas - 1) / total
       const int c0 = (int)(((seg0 + 1) * ctas - 1) / total), c1 = (int)(((seg0 + st.count) * ctas - 1) / total);
-      __syncthreads();
-      if (tid == 0) arrived = atom_add_acq_rel_gpu(A.counters + c0, 1u);
-      __syncthreads();
-      if (arrived == (uint32_t)(c1 - c0)) {
+      const int n = c1 - c0 + 1;
+      auto slot_of = [&](int b) { return A.ws + (size_t)(2 * b + (b == c0 ? 1 : 0)) * kSlot; };
+      // The last of the CTAs joins their results, from as many as fit one round of loads; more
+      // are joined in about sqrt(n) groups first, each by its own last.
+      auto last_of = [&](uint32_t* counter, int of) {
+        __syncthreads();
+        if (tid == 0) arrived = atom_add_acq_rel_gpu(counter, 1u);
+        __syncthreads();
+        if (arrived != (uint32_t)(of - 1)) return false;
         __threadfence();
-        for (int k = tid; k < rows * D; k += kDecThreads) {
-          const int row = k / D, d = k - row * D;
-          float M = -INFINITY, L = 0.f, O = 0.f;
-          for (int b = c0; b <= c1; ++b)
-            M = fmaxf(M, __ldcg(A.ws + (size_t)(2 * b + (b == c0 ? 1 : 0)) * kSlot + R * D + row));
-          const float mm = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-          for (int b = c0; b <= c1; ++b) {
-            const float* p = A.ws + (size_t)(2 * b + (b == c0 ? 1 : 0)) * kSlot;
-            const float f = exp2_fast(__ldcg(p + R * D + row) - mm);
-            L = fmaf(f, __ldcg(p + R * D + R + row), L);
-            O = fmaf(f, __ldcg(p + k), O);
-          }
-          const int tok = row / A.group, hh = row - tok * A.group;
-          A.out[(size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D + d] =
-              __float2half_rn(L == 0.f ? 0.f : O / L);
+        if (tid == 0) *counter = 0u;
+        return true;
+      };
+      auto join = [&](int b0, int step, int cnt, bool final) {
+        for (int k = tid; k < cnt * rows; k += kDecThreads) {
+          const float* p = slot_of(b0 + (k / rows) * step) + R * D + k % rows;
+          j_m[k / rows][k % rows] = __ldcg(p);
+          j_l[k / rows][k % rows] = __ldcg(p + R);
         }
-        if (tid == 0) A.counters[c0] = 0u;
+        __syncthreads();
+        float M = -INFINITY, L = 0.f;
+        if (tid < rows) {
+          for (int b = 0; b < cnt; ++b) M = fmaxf(M, j_m[b][tid]);
+          const float mm = M == -INFINITY ? 0.f : M;
+          for (int b = 0; b < cnt; ++b) {
+            const float f = exp2_fast(j_m[b][tid] - mm);
+            j_m[b][tid] = f;
+            L = fmaf(f, j_l[b][tid], L);
+          }
+          j_l[0][tid] = L;
+        }
+        __syncthreads();
+        float* dst = slot_of(b0);
+        for (int k = 4 * tid; k < rows * D; k += 4 * kDecThreads) {
+          const int row = k / D, d = k - row * D;
+          float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+          for (int b = 0; b < cnt; ++b) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(slot_of(b0 + b * step) + k));
+            const float f = j_m[b][row];
+            O.x = fmaf(f, v.x, O.x);
+            O.y = fmaf(f, v.y, O.y);
+            O.z = fmaf(f, v.z, O.z);
+            O.w = fmaf(f, v.w, O.w);
+          }
+          if (final) {
+            const float sum = j_l[0][row], r = sum == 0.f ? 0.f : __frcp_rn(sum);
+            const int tok = row / A.group, hh = row - tok * A.group;
+            __half* y = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D + d;
+            *reinterpret_cast<uint2*>(y) = make_uint2(pack_half2(O.x * r, O.y * r), pack_half2(O.z * r, O.w * r));
+          } else {
+            *reinterpret_cast<float4*>(dst + k) = O;
+          }
+        }
+        if (!final && tid < rows) {
+          dst[R * D + tid] = M;
+          dst[R * D + R + tid] = L;
+        }
+      };
+      int per = n;
+      if (n > kDecJoin) {
+        per = 1;
+        while (per * per < n) ++per;
+        const int b0 = c0 + ((int)blockIdx.x - c0) / per * per, cnt = c1 - b0 + 1 < per ? c1 - b0 + 1 : per;
+        // (a CTA may start one group of an earlier head and the first group of its last head)
+        if (!last_of(A.counters + (b0 == c0 ? 2 : 1) * gridDim.x + b0, cnt)) per = 0;
+        if (per) join(b0, 1, cnt, false);
       }
+      if (per && last_of(A.counters + c0, n > kDecJoin ? (n + per - 1) / per : n))
+        join(c0, n > kDecJoin ? per : 1, n > kDecJoin ? (n + per - 1) / per : n, true);
     }
     __syncthreads();
 
@@ -470,7 +532,11 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
 template <int D, int RT>
 static cudaError_t launch_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {
   const auto fn = kv8_decode_kernel<D, RT>;
-  const size_t smem = sizeof(float) * kDecWarps * (8 * RT * D + 2 * 8 * RT);
+  const size_t smem = sizeof(Ring<D>) * kDecWarps;
+  const cudaError_t e = ensure_max_dyn_smem(fn);
+  if (e != cudaSuccess) return e;
+  static_assert(kDecodeCtas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)
+  if (num_sms > 256) return cudaErrorInvalidValue;
   fn<<<num_sms * (RT == 1 ? kDecodeCtas8 : kDecodeCtas16), kDecThreads, smem, s>>>(a);
   return cudaGetLastError();
 }
