@@ -9,13 +9,14 @@
 // Inside a CTA the warps take every fourth step; each keeps its own running maximum, sum and
 // accumulators, joined through shared memory once per share.
 //
-// A warp multiplies with 16 x 8 x 16 register MMAs (rows of q x keys, then rows x dims): with
-// one row tile of at most 16 rows there is nothing for tcgen05's 128-row tiles to do.  Each
-// warp keeps its own ring of steps in shared memory, filled by asynchronous 16-byte copies
-// (no barrier between warps), and reads fragments in whatever order suits 16-byte reads:
-//   * logits: the B fragment of key g takes any order of the dims as long as q has the same,
-//     so a lane takes 16 consecutive bytes of its key's row at a time;
-//   * values: the B fragment of dim g takes any order of the dims across its tiles, so a lane
+// A warp multiplies with 16 x 8 x 16 register MMAs, codes first (keys x rows of q, then dims x
+// rows: eight rows are then no padding): with at most 16 rows there is nothing for tcgen05's
+// 128-row tiles to do.  Each warp keeps its own ring of steps in shared memory, filled by
+// asynchronous 16-byte copies (no barrier between warps), and reads fragments in whatever
+// order suits 16-byte reads:
+//   * logits: the A fragment of key g takes any order of the dims as long as q has the same,
+//     so a lane takes 16 consecutive bytes of its keys' rows at a time;
+//   * values: the A fragment of dim g takes any order of the dims across its tiles, so a lane
 //     takes D / 8 consecutive bytes of four keys.
 // Each 16-byte chunk of a 128-byte line stands at its place xor the line's number mod 8, so
 // that neither read meets a bank twice.
@@ -131,7 +132,13 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool on) {
 // Where byte `at` (a multiple of 8) of a half of a step stands.
 __device__ __forceinline__ uint32_t swz(uint32_t at) { return at ^ (((at >> 7) & 7u) << 4); }
 
-template <int D, int RT>   // RT: 8-row halves of the row tile that hold rows (1 or 2)
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {   // of binary16, two of a row in each lane
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <int D, int RT>   // RT: tiles of 8 rows (1 or 2)
 __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeCtas16) kv8_decode_kernel(const Kv8AttendArgs A) {
   constexpr int VB = D / 8;                       // bytes of a V row for one lane; n-tiles of the second product
   constexpr int R = 8 * RT, kSlot = R * D + 2 * R;   // floats of a partial result
@@ -201,28 +208,36 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
     const int rows = q.n * A.group;
 
     // ---- this share's rows of q, in the order of the dims that the keys' bytes have
-    uint32_t qf[D / 16][2 * RT];
-    int pos[RT];
+    uint32_t qf[RT][D / 16][2];
+    int pos[RT][2];   // positions of the two rows whose logits this lane holds
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int row = g + 8 * r, tok = row / A.group, hh = row - tok * A.group;
-      pos[r] = row < rows ? q.start + tok : -1;
       const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint2 v = make_uint2(0u, 0u);
         if (row < rows) v = __ldg(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
-        qf[k][r] = v.x;
-        qf[k][RT + r] = v.y;
+        qf[r][k][0] = v.x;
+        qf[r][k][1] = v.y;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int mine = 8 * r + 2 * t + e;
+        pos[r][e] = mine < rows ? q.start + mine / A.group : -1;
       }
     }
-    float o[VB][2 * RT], m[RT], l[RT];
+    // weighted values of two rows, dims VB g + 2 j and the next
+    float o[RT][VB / 2][4], m[RT][2], l[RT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) m[r] = -INFINITY, l[r] = 0.f;
+    for (int r = 0; r < RT; ++r) {
+      m[r][0] = m[r][1] = -INFINITY;
+      l[r][0] = l[r][1] = 0.f;
 #pragma unroll
-    for (int j = 0; j < VB; ++j)
+      for (int j = 0; j < VB / 2; ++j)
 #pragma unroll
-      for (int e = 0; e < 2 * RT; ++e) o[j][e] = 0.f;
+        for (int e = 0; e < 4; ++e) o[r][j][e] = 0.f;
+    }
 
     // ---- the steps of this warp
     auto key_of = [&](int i) { return i < st.sink ? i * kDecKeys : st.from + (i - st.sink) * kDecKeys; };
@@ -275,120 +290,119 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
       const bool held0 = ring.blk[stage][0] >= 0, held1 = ring.blk[stage][1] >= 0;
       const float4 scl = *reinterpret_cast<const float4*>(ring.scale[stage]);
       const int key = key_of(i);
-      float sc[4][4];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
-        uint4 kw[D / 64];
-#pragma unroll
-        for (int ch = 0; ch < D / 64; ++ch)
-          kw[ch] = *reinterpret_cast<const uint4*>(sk + swz((8 * n + g) * D + D / 4 * t + 16 * ch));
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint4& w4 = kw[k >> 2];
-          const uint32_t w = (k & 3) == 0 ? w4.x : (k & 3) == 1 ? w4.y : (k & 3) == 2 ? w4.z : w4.w;
-          uint32_t b0, b1;
-          widen4(w, b0, b1);
-          if constexpr (RT == 1)
-            mma_16816(sc[n], qf[k][0], 0u, qf[k][1], 0u, b0, b1);
-          else
-            mma_16816(sc[n], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b0, b1);
-        }
-      }
-      // x_j, per 16 keys one factor and one addend
-      float fa[2], fb[2], inv[2];
+      // logits of 16 keys and 8 rows: keys g, g + 8, rows 2 t, 2 t + 1
+      float x[2][RT][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float v = fmaxf(h ? scl.w : scl.z, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-        fa[h] = (h ? scl.y : scl.x) * (A.scale * 1.4426950408889634f);
-        fb[h] = __log2f(v);
-        inv[h] = __frcp_rn(v);
-      }
-      float top[RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) top[r] = m[r];
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[h][r][e] = 0.f;
+#pragma unroll
+        for (int ch = 0; ch < D / 64; ++ch) {
+          const uint4 k0 = *reinterpret_cast<const uint4*>(sk + swz((16 * h + g) * D + D / 4 * t + 16 * ch));
+          const uint4 k1 = *reinterpret_cast<const uint4*>(sk + swz((16 * h + 8 + g) * D + D / 4 * t + 16 * ch));
+          const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t a0, a1, a2, a3;
+            widen4(w0[k], a0, a2);
+            widen4(w1[k], a1, a3);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) mma_16816(x[h][r], a0, a1, a2, a3, qf[r][4 * ch + k][0], qf[r][4 * ch + k][1]);
+          }
+        }
+      }
       // every row sees every key of the step
       const bool all = held0 && held1 && key + kDecKeys - 1 <= q.start &&
                        (A.window == 0 || key > q.len - 1 - A.window || key + kDecKeys <= A.sinks);
+      float inv[2], top[RT][2];
 #pragma unroll
-      for (int n = 0; n < 4; ++n)
+      for (int r = 0; r < RT; ++r) top[r][0] = m[r][0], top[r][1] = m[r][1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {   // per 16 keys one factor and one addend
+        const float v = fmaxf(h ? scl.w : scl.z, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
+        const float fa = (h ? scl.y : scl.x) * (A.scale * 1.4426950408889634f), fb = __log2f(v);
+        inv[h] = __frcp_rn(v);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[h][r][e] = fmaf(x[h][r][e], fa, fb);
+      }
+      if (!all) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!((h ? held1 : held0) &&
+                    kv8_sees(pos[r][e & 1], key + 16 * h + g + 8 * (e >> 1), A.window, A.sinks)))
+                x[h][r][e] = -INFINITY;
+      }
+      bool grown = false;
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float v = fmaxf(fmaxf(x[0][r][e], x[0][r][e + 2]), fmaxf(x[1][r][e], x[1][r][e + 2]));
+          grown |= v > m[r][e];
+          top[r][e] = fmaxf(v, m[r][e]);
+        }
+      if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float& v = sc[n][2 * r + e];
-            v = fmaf(v, fa[n >> 1], fb[n >> 1]);
-            if (!all) {
-              const int j = key + 8 * n + 2 * t + e;
-              if (!((n < 2 ? held0 : held1) && kv8_sees(pos[r], j, A.window, A.sinks))) v = -INFINITY;
-            }
-            top[r] = fmaxf(top[r], v);
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) top[r][e] = fmaxf(top[r][e], __shfl_xor_sync(0xffffffffu, top[r][e], w));
+            const float f = top[r][e] == m[r][e] ? 1.f : exp2_fast(m[r][e] - top[r][e]);
+            m[r][e] = top[r][e];
+            l[r][e] *= f;
+#pragma unroll
+            for (int j = 0; j < VB / 2; ++j) o[r][j][e] *= f, o[r][j][e + 2] *= f;
           }
+      }
+      uint32_t pf[2][RT][2];   // B fragments of the weights, per 16 keys
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-        if (__any_sync(0xffffffffu, top[r] != m[r])) {
-          const float f = top[r] == m[r] ? 1.f : exp2_fast(m[r] - top[r]);
-          l[r] *= f;
+        const float m0 = m[r][0] == -INFINITY ? 0.f : m[r][0], m1 = m[r][1] == -INFINITY ? 0.f : m[r][1];
 #pragma unroll
-          for (int j = 0; j < VB; ++j) o[j][2 * r] *= f, o[j][2 * r + 1] *= f;
-          m[r] = top[r];
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = exp2_fast(x[h][r][0] - m0), p1 = exp2_fast(x[h][r][1] - m1);
+          const float p2 = exp2_fast(x[h][r][2] - m0), p3 = exp2_fast(x[h][r][3] - m1);
+          l[r][0] = fmaf(p0 + p2, inv[h], l[r][0]);
+          l[r][1] = fmaf(p1 + p3, inv[h], l[r][1]);
+          pf[h][r][0] = transpose8x8(pack_half2(p0, p1));
+          pf[h][r][1] = transpose8x8(pack_half2(p2, p3));
         }
       }
-      uint32_t pf[2][2 * RT];   // A fragments of the weights, per 16 keys
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        uint32_t vw[4][VB / 4];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const float mm = m[r] == -INFINITY ? 0.f : m[r];
-          float p[4], sum = 0.f;
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              p[2 * u + e] = exp2_fast(sc[2 * h + u][2 * r + e] - mm);
-              sum += p[2 * u + e];
-            }
-          l[r] = fmaf(sum, inv[h], l[r]);
-          pf[h][r] = pack_half2(p[0], p[1]);
-          pf[h][RT + r] = pack_half2(p[2], p[3]);
-        }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-{
-          uint32_t vw[4][VB / 4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint8_t* p = sv + swz((16 * h + 2 * t + (u >> 1) * 8 + (u & 1)) * D + VB * g);
-            if constexpr (D == 128) {
-              const uint4 v = *reinterpret_cast<const uint4*>(p);
-              vw[u][0] = v.x, vw[u][1] = v.y, vw[u][2] = v.z, vw[u][3] = v.w;
-            } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(p);
-              vw[u][0] = v.x, vw[u][1] = v.y;
-            }
-          }
-#pragma unroll
-          for (int w = 0; w < VB / 4; ++w) {
-            uint32_t b0[4], b1[4];
-            widen_pairs(vw[0][w], vw[1][w], b0);
-            widen_pairs(vw[2][w], vw[3][w], b1);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float (&acc)[2 * RT] = o[4 * w + e];
-              if constexpr (RT == 1) {
-                float d[4] = {acc[0], acc[1], 0.f, 0.f};
-                mma_16816(d, pf[h][0], 0u, pf[h][1], 0u, b0[e], b1[e]);
-                acc[0] = d[0];
-                acc[1] = d[1];
-              } else {
-                mma_16816(acc, pf[h][0], pf[h][1], pf[h][2], pf[h][3], b0[e], b1[e]);
-              }
-            }
+        for (int u = 0; u < 4; ++u) {   // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+          const uint8_t* p = sv + swz((16 * h + 2 * t + (u >> 1) * 8 + (u & 1)) * D + VB * g);
+          if constexpr (D == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            vw[u][0] = v.x, vw[u][1] = v.y, vw[u][2] = v.z, vw[u][3] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            vw[u][0] = v.x, vw[u][1] = v.y;
           }
         }
+#pragma unroll
+        for (int w = 0; w < VB / 4; ++w) {
+          uint32_t a[4], b[4];
+          widen_pairs(vw[0][w], vw[1][w], a);
+          widen_pairs(vw[2][w], vw[3][w], b);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            mma_16816(o[r][2 * w], a[0], a[1], b[0], b[1], pf[h][r][0], pf[h][r][1]);
+            mma_16816(o[r][2 * w + 1], a[2], a[3], b[2], b[3], pf[h][r][0], pf[h][r][1]);
+          }
+        }
+      }
       __syncwarp();
       issue(i + NS * kDecWarps, stage, blk);
       stage = stage + 1 == NS ? 0 : stage + 1;
@@ -398,20 +412,20 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
 
     // ---- the CTA's warps joined
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-      float* dst = reinterpret_cast<float*>(&ring) + (g + 8 * r) * D;
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int j = 0; j < VB; ++j) {
-        dst[2 * t * VB + j] = o[j][2 * r];
-        dst[(2 * t + 1) * VB + j] = o[j][2 * r + 1];
+      for (int e = 0; e < 2; ++e) {
+        const int row = 8 * r + 2 * t + e;
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], w);
+        float* dst = reinterpret_cast<float*>(&ring) + row * D + VB * g;
+#pragma unroll
+        for (int j = 0; j < VB / 2; ++j) *reinterpret_cast<float2*>(dst + 2 * j) = make_float2(o[r][j][e], o[r][j][e + 2]);
+        if (g == 0) {
+          s_m[warp][row] = m[r][e];
+          s_l[warp][row] = l[r][e];
+        }
       }
-      if (t == 0) {
-        s_m[warp][g + 8 * r] = m[r];
-        s_l[warp][g + 8 * r] = l[r];
-      }
-    }
     __syncthreads();
     const bool whole = i0 == 0 && i1 == st.count;
     const long long seg0 = it - i0;   // the (sequence, head)'s steps: seg0 .. seg0 + count - 1
