@@ -246,7 +246,8 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
  * largest so far; logits, maxima, sums and accumulators are fp32.
  * q_fp16, out_fp16: device rows of `tokens` tokens, q_heads * head_dim binary16 values each, rows
  * q_stride / out_stride elements apart; 16-byte aligned, strides multiples of 8.
- * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.
+ * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.  max_tokens at
+ * most 65535 (UNSUPPORTED).
  * Asynchronous; uses the library's per-device scratch (allocated by the first call, or by
  * dptq_kv8_reserve).  Errors as dptq_kv8_append. */
 dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,

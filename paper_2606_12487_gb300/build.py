@@ -31,7 +31,7 @@ if DEBUG:
     OUT_DIR = os.path.join(HERE, "_build_debug")
     LIB = os.path.join(OUT_DIR, "libdptq.so")
 SOURCES = ["api.cu", "rotate_quant.cu", "qgemm.cu", "static_scratch.cu", "kv_policy.cu", "norm_quant.cu",
-           "kv8_append.cu", "kv8_decode.cu", "kv8_attend.cu"]
+           "kv8_append.cu", "kv8_decode.cu", "kv8_prefill.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

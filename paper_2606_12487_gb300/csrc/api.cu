@@ -850,6 +850,7 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (q_heads <= 0 || window < 0 || sinks < 0 || !std::isfinite(scale))
     return fail(DPTQ_ERR_INVALID_ARG, "bad q_heads, window, sinks or scale");
+  if (batch && batch->max_tokens > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "more than 65535 rows of a sequence in one call");
   if (cache && cache->kv_heads > 0) {
     if (q_heads % cache->kv_heads != 0) return fail(DPTQ_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
     if (q_heads / cache->kv_heads > 64) return fail(DPTQ_ERR_UNSUPPORTED, "more than 64 query heads for a KV head");
@@ -873,8 +874,9 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   if ((st = ensure_kv8_scratch(sc, s)) != DPTQ_OK) return st;
   a.ws = sc->kv8_ws;
   a.counters = sc->kv8_counters;
+  a.wait_cycles = wait_cycles_setting();
   const bool decode = (long long)a.c.max_tokens * a.group <= kDecodeRows;
-  DPTQ_CUDA(decode ? launch_kv8_decode(a, sc->num_sms, s) : launch_kv8_attend(a, sc->num_sms, s), "kv8_attention launch");
+  DPTQ_CUDA(decode ? launch_kv8_decode(a, sc->num_sms, s) : launch_kv8_prefill(a, sc->num_sms, s), "kv8_attention launch");
   return DPTQ_OK;
 }
 

@@ -35,7 +35,7 @@ namespace dptq {
 
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 constexpr int kDecKeys = 32;        // keys of a step
-constexpr int kDecMinSteps = 16;    // fewest steps that a CTA is started for
+constexpr int kDecMinSteps = 4;     // fewest steps that a CTA is started for: one a warp
 constexpr int kDecJoin = 12;        // most partial results joined at once
 constexpr int kDecJoinMost = 32;    // of a group, and groups: sqrt of a grid of 1024 CTAs at most
 
@@ -46,21 +46,6 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t less_1152(uint32_t h) {
-  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2half2(__ushort_as_half(0x6480)));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-// Four codes to two pairs of binary16: values 0, 1 and 2, 3.
-__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  w ^= 0x80808080u;
-  lo = less_1152(__byte_perm(w, 0x64646464u, 0x4140));
-  hi = less_1152(__byte_perm(w, 0x64646464u, 0x4342));
-}
 // Four codes of two keys to four pairs (key a, key b).
 __device__ __forceinline__ void widen_pairs(uint32_t a, uint32_t b, uint32_t (&r)[4]) {
   const uint32_t lo = __byte_perm(a, b, 0x5140) ^ 0x80808080u, hi = __byte_perm(a, b, 0x7362) ^ 0x80808080u;
@@ -69,10 +54,10 @@ __device__ __forceinline__ void widen_pairs(uint32_t a, uint32_t b, uint32_t (&r
   r[2] = less_1152(__byte_perm(hi, 0x64646464u, 0x4140));
   r[3] = less_1152(__byte_perm(hi, 0x64646464u, 0x4342));
 }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
+// What a (sequence, head) costs a CTA beyond its steps (its rows of q, the first copies' latency,
+// the join): shares of 16 steps and more are cut as if every one had so many steps more, which
+// come first.  32 ragged MHA sequences (7 to 128 steps a head): 124 us without, 100 us with 6 or 10.
+constexpr int kDecExtra = 6, kDecExtraFrom = 16;
 
 // The steps of a sequence: `sink` steps from key 0, then steps from key `from`.
 struct Steps {
@@ -156,6 +141,7 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
 
   // ---- this CTA's share
   long long total = 0;
+  int some = 0;   // sequences with steps
   bool none = false;   // a sequence of rows without a key
   for (int s0 = 0; s0 < c.seqs; s0 += kDecThreads) {
     Seq q;
@@ -166,10 +152,13 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
     }
     block_scan(n, red, all);
     total += all;
+    some += __syncthreads_count(n > 0);
   }
   total *= c.kv_heads;
   long long ctas = (total + kDecMinSteps - 1) / kDecMinSteps;
   if (ctas > gridDim.x) ctas = gridDim.x;
+  const int extra = total >= (long long)kDecExtraFrom * ctas ? kDecExtra : 0;
+  total += (long long)extra * some * c.kv_heads;
   // (such a sequence has no step: zeros, from CTA 0)
   if (blockIdx.x == 0 && __syncthreads_or(none)) {
     for (int s = 0; s < c.seqs; ++s) {
@@ -188,6 +177,7 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
     Seq q;
     int n = 0, all;
     if (s0 + tid < c.seqs && load_seq(c, s0 + tid, q, false)) n = seq_steps(q, A.window, A.sinks).count;
+    n += n > 0 ? extra : 0;
     const long long at = before + (long long)block_scan(n, red, all) * c.kv_heads;
     if (n > 0 && at <= begin && begin < at + (long long)n * c.kv_heads) {
       found[0] = s0 + tid;
@@ -198,13 +188,15 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
     __syncthreads();
     if (before > begin) break;
   }
-  int s = found[0], head = found[1], i0 = found[2];
+  int s = found[0], head = found[1], v0 = found[2];   // (v: steps with the extra ones)
 
   Seq q;
   load_seq(c, s, q, false);
   Steps st = seq_steps(q, A.window, A.sinks);
   for (long long it = begin; it < end;) {
-    const int i1 = (int)(end - it < st.count - i0 ? i0 + (end - it) : st.count);
+    const int vs = st.count + extra, v1 = (int)(end - it < vs - v0 ? v0 + (end - it) : vs);
+    const int i0 = v0 > extra ? v0 - extra : 0, i1 = v1 - extra;
+    if (i1 > i0) {
     const int rows = q.n * A.group;
 
     // ---- this share's rows of q, in the order of the dims that the keys' bytes have
@@ -428,7 +420,7 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
       }
     __syncthreads();
     const bool whole = i0 == 0 && i1 == st.count;
-    const long long seg0 = it - i0;   // the (sequence, head)'s steps: seg0 .. seg0 + count - 1
+    const long long seg0 = it - v0 + extra;   // the (sequence, head)'s steps: seg0 .. seg0 + count - 1
     float* slot = A.ws + (size_t)(2 * blockIdx.x + (i0 == 0 ? 1 : 0)) * kSlot;
     for (int k = tid; k < rows * D; k += kDecThreads) {
       const int row = k / D, d = k - row * D;
@@ -529,10 +521,11 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
         join(c0, n > kDecJoin ? per : 1, n > kDecJoin ? (n + per - 1) / per : n, true);
     }
     __syncthreads();
+    }
 
     // ---- on to the next (sequence, head)
-    it += i1 - i0;
-    i0 = 0;
+    it += v1 - v0;
+    v0 = 0;
     if (it < end && ++head == c.kv_heads) {
       head = 0;
       do {

@@ -49,4 +49,24 @@ __device__ __forceinline__ int quant_code(float x, float s) {
   return s > 0.f ? __float2int_rn(__fdiv_rn(x, s)) : 0;
 }
 
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t less_1152(uint32_t h) {
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h), __half2half2(__ushort_as_half(0x6480)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Four codes to two pairs of binary16: values 0, 1 and 2, 3.
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  w ^= 0x80808080u;
+  lo = less_1152(__byte_perm(w, 0x64646464u, 0x4140));
+  hi = less_1152(__byte_perm(w, 0x64646464u, 0x4342));
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
 }  // namespace dptq

@@ -1,0 +1,515 @@
+// kv8_prefill.cu -- attention of many rows (prompts, chunks of prompts, more than 16 rows of a
+// sequence and KV head) over the paged int8 cache, on the 5th-generation tensor cores.
+//
+// The rows of a KV head (a token's query heads side by side, then the next token's) are cut
+// into tiles of 256; a CTA takes two row tiles of 128 so that one's softmax runs while the
+// tensor cores work for the other, and both share every widened K and V tile of 128 keys:
+//   S = q ck^T   128 x 128 x D   both operands in shared memory, S in tensor memory
+//   O += P cv    128 x D x 128   P in tensor memory (over S), cv in shared memory
+// The codes enter the MMAs as they are (int8 is exact in binary16); scales and the softmax in
+// base 2 are as in the decode kernel: x_j = log2(e) scale sk S_j + log2(sv), weights p_j sv_j
+// relative to the row's maximum, the denominator taken back by 1 / sv, per 16 keys of a page.
+// O is rescaled only where a row's maximum has grown by more than 2^8 (binary16 holds the
+// weights that stay relative to the old one).
+//
+// Warp roles: 0-3 and 4-7 softmax and output of the row tiles, a row a thread; 8-11 widen K and
+// V tiles (global to registers a tile ahead, then to shared memory in the 128-byte swizzle);
+// 12 issues the MMAs.
+//
+// Few row tiles are split along the keys: each CTA leaves its rows' sums, and a second launch
+// joins them.
+#include <cstdint>
+#include <cuda_runtime.h>
+#include <cuda_fp16.h>
+
+#include "kv8_device.cuh"
+
+namespace dptq {
+
+constexpr int kPreThreads = 512, kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
+
+struct KeyMeta {     // of 16 keys
+  float a, b, inv;   // x = a S + b; 1 / sv
+  float pad;
+};
+struct PreShared {
+  KeyMeta meta[kMeta][kTileKeys / 16];
+  uint64_t kfull[kPreStages], kempty[kPreStages], vfull[kPreStages], vempty[kPreStages];
+  uint64_t qfull[2], sfull[2], pfull[2], ofull[2], drain;
+  uint32_t tmem;
+  int abort;
+};
+
+// D[tmem] (+)= A B^T, binary16 operands, fp32 accumulators: A in shared memory or tensor memory.
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: binary16 operands, fp32 accumulators, 128 rows; b_mn: B's rows (N)
+// are contiguous instead of its K.
+__host__ __device__ constexpr uint32_t idesc_f16(int n, bool b_mn) {
+  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+// B with contiguous N in the 128-byte swizzle: atoms of 64 n x 8 k, 1024 bytes apart along k,
+// `n_stride` bytes apart along n.
+__device__ __forceinline__ uint64_t sdesc_mn128(uint32_t saddr, uint32_t n_stride) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(n_stride >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
+        "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
+        "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(taddr));
+}
+template <int N>
+__device__ __forceinline__ void reg_more() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_less() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// The 128-key tiles that a CTA's rows see: `sink` tiles from key 0, then tiles from key `from`.
+struct Tiles {
+  int sink, from, count;
+  __device__ __forceinline__ int key(int j) const { return j < sink ? j * kTileKeys : from + (j - sink) * kTileKeys; }
+};
+__device__ __forceinline__ Tiles row_tiles(int p_lo, int p_hi, int window, int sinks) {   // positions of the rows
+  Tiles r{0, 0, 0};
+  if (p_hi < 0) return r;
+  if (window > 0) {
+    const int first = (p_lo > 0 ? p_lo : 0) - window + 1;
+    if (first >= kTileKeys) {
+      r.from = first & ~(kTileKeys - 1);
+      r.sink = sinks < r.from ? (sinks + kTileKeys - 1) / kTileKeys : r.from / kTileKeys;
+    }
+  }
+  r.count = r.sink + (p_hi + 1 - r.from + kTileKeys - 1) / kTileKeys;
+  return r;
+}
+
+template <int D>
+struct PreLayout {
+  static constexpr int kHalf = 128 * 128;               // 64 dims (or 64-dim group) x 128 rows
+  static constexpr int kTile = D / 64 * kHalf;          // a widened tile, or a row tile of q
+  static constexpr int kQ = 0, kK = 2 * kTile, kV = kK + kPreStages * kTile, kEnd = kV + kPreStages * kTile;
+  static constexpr int kBytes = kEnd + (int)sizeof(PreShared) + 1024;   // (1024: alignment)
+};
+
+// SPLIT: this CTA's part of the keys goes to the scratch, for kv8_join_kernel.
+template <int D, bool SPLIT>
+__global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8AttendArgs A, int nsplit) {
+  using L = PreLayout<D>;
+  extern __shared__ uint8_t raw[];
+  uint8_t* sm = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  PreShared& S = *reinterpret_cast<PreShared*>(sm + L::kEnd);
+  const Kv8Args& c = A.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int head = blockIdx.x, seq = blockIdx.y;
+  const int split = SPLIT ? blockIdx.z % nsplit : 0, zt = SPLIT ? blockIdx.z / nsplit : blockIdx.z;
+  Seq q;
+  if (!load_seq(c, seq, q, tid == 0 && blockIdx.z == 0 && head == 0)) return;
+  const int rows = q.n * A.group;
+  const int tile = (rows + 2 * kTileRows - 1) / (2 * kTileRows) - 1 - zt;   // the last rows, with the most keys, first
+  if (tile < 0) return;
+  const int row0 = tile * 2 * kTileRows, nrows = rows - row0 < 2 * kTileRows ? rows - row0 : 2 * kTileRows;
+  const int halves = nrows > kTileRows ? 2 : 1;
+  const int p_first = q.start + row0 / A.group, p_last = q.start + (row0 + nrows - 1) / A.group;
+  const Tiles all = row_tiles(p_first, p_last, A.window, A.sinks);
+  const int j0 = SPLIT ? (int)((long long)all.count * split / nsplit) : 0;
+  const int nt = (SPLIT ? (int)((long long)all.count * (split + 1) / nsplit) : all.count) - j0;
+
+  if (tid == 0) {
+    for (int i = 0; i < kPreStages; ++i) {
+      mbar_init(&S.kfull[i], 4);
+      mbar_init(&S.vfull[i], 4);
+      mbar_init(&S.kempty[i], 1);
+      mbar_init(&S.vempty[i], 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&S.qfull[t], kTileRows);
+      mbar_init(&S.pfull[t], kTileRows);
+      mbar_init(&S.sfull[t], 1);
+      mbar_init(&S.ofull[t], 1);
+    }
+    mbar_init(&S.drain, 1);
+    S.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 12) tmem_alloc<false>(&S.tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = S.tmem;   // S of the row tiles at columns 0 and 128, O at 256 and 384
+  volatile int* abort_flag = &S.abort;
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax, a row a thread
+    reg_more<184>();
+    const int t = warp >> 2, r = tid & (kTileRows - 1), row = row0 + t * kTileRows + r;
+    const bool mine = row < row0 + nrows;
+    const int tok = row / A.group, hh = row - tok * A.group;
+    const int pos = mine ? q.start + tok : -1;
+    const uint32_t tlane = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tm + tlane + t * 128, tO = tm + tlane + 256 + t * 128;
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    if (t < halves && nt > 0) {
+      {   // this row of q, negated for a negative scale
+        const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
+        const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D;
+        uint8_t* dst = sm + L::kQ + t * L::kTile + r * 128;
+#pragma unroll
+        for (int ch = 0; ch < D / 8; ++ch) {
+          uint4 v = mine ? __ldg(reinterpret_cast<const uint4*>(src) + ch) : make_uint4(0u, 0u, 0u, 0u);
+          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+          *reinterpret_cast<uint4*>(dst + (ch >> 3) * L::kHalf + (((ch & 7) ^ (r & 7)) << 4)) = v;
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(&S.qfull[t]);
+      }
+      // positions of this row tile's rows
+      const int p_lo = q.start + (row0 + t * kTileRows) / A.group;
+      const int last = t == halves - 1 ? nrows - 1 : kTileRows - 1, p_hi = q.start + (row0 + last) / A.group;
+      for (int j = 0; j < nt && ok; ++j) {
+        ok = mbar_wait_warp(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+        if (!ok) break;
+        tc_fence_after();
+        float x[kTileKeys];
+#pragma unroll
+        for (int k = 0; k < kTileKeys; k += 32) tmem_ld32(tS + k, x + k);
+        tmem_ld_wait();
+        const int key = all.key(j0 + j);
+        const bool seen = key + kTileKeys - 1 <= p_lo &&
+                          (A.window == 0 || key > p_hi - A.window || key + kTileKeys <= A.sinks);
+        if (!seen) {
+#pragma unroll
+          for (int k = 0; k < kTileKeys; ++k)
+            if (!kv8_sees(pos, key + k, A.window, A.sinks)) x[k] = -INFINITY;
+        }
+        const KeyMeta* meta = S.meta[j % kMeta];
+        float top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < kTileKeys / 16; ++g) {
+          float v = x[16 * g];
+#pragma unroll
+          for (int k = 1; k < 16; ++k) v = fmaxf(v, x[16 * g + k]);
+          top = fmaxf(top, fmaf(v, meta[g].a, meta[g].b));
+        }
+        if (__any_sync(0xffffffffu, top > m + 8.f)) {   // (m = -inf: the row's first keys)
+          const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);
+          m = mn;
+          l *= f;
+          if (j > 0) {   // (PV of tile j - 1 came before S of tile j, which is here)
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+              float o[32];
+              tmem_ld32(tO + k, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] *= f;
+              tmem_st32(tO + k, reinterpret_cast<const uint32_t(&)[32]>(o));
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[32];
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const KeyMeta& mt = meta[4 * h + g];
+            const float a = mt.a, b = mt.b - base;
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              const float p0 = exp2_fast(fmaf(x[64 * h + 16 * g + k], a, b));
+              const float p1 = exp2_fast(fmaf(x[64 * h + 16 * g + k + 1], a, b));
+              sum += p0 + p1;
+              p[8 * g + k / 2] = pack_half2(p0, p1);
+            }
+            l = fmaf(sum, mt.inv, l);
+          }
+          tmem_st32(tS + 32 * h, p);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&S.pfull[t]);
+      }
+      if (ok) ok = mbar_wait_warp(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+      tc_fence_after();
+    }
+    // ---- output
+    if (ok && t < halves) {
+      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+      __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D;
+      float* part = nullptr;
+      if constexpr (SPLIT) {
+        part = A.ws + ((((size_t)seq * (gridDim.z / nsplit) + tile) * gridDim.x + head) * nsplit + split) *
+                          (2 * kTileRows * (D + 2));
+        if (mine) {
+          part[2 * kTileRows * D + t * kTileRows + r] = m;
+          part[2 * kTileRows * (D + 1) + t * kTileRows + r] = l;
+        }
+        part += (size_t)(t * kTileRows + r) * D;
+      }
+#pragma unroll
+      for (int k = 0; k < D; k += 32) {
+        float o[32];
+        if (nt > 0) {
+          tmem_ld32(tO + k, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (mine) {
+          if constexpr (SPLIT) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(part + k + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              *reinterpret_cast<uint4*>(dst + k + e) =
+                  make_uint4(pack_half2(o[e] * inv, o[e + 1] * inv), pack_half2(o[e + 2] * inv, o[e + 3] * inv),
+                             pack_half2(o[e + 4] * inv, o[e + 5] * inv), pack_half2(o[e + 6] * inv, o[e + 7] * inv));
+          }
+        }
+      }
+    }
+    tc_fence_before();
+  } else if (warp < 12) {
+    // ------------------------------------------------------------------ K and V, widened
+    reg_less<104>();
+    const int w = warp - 8, sub = D == 128 ? w & 1 : 0, kr = lane >> 2, col = lane & 3;
+    constexpr int kWays = D == 128 ? 2 : 4;              // 8-key blocks side by side
+    constexpr int kUnits = 16 / kWays;                   // blocks of a warp: 8 or 4
+    const int kb0 = D == 128 ? w >> 1 : w;
+    const int P1 = (1 << c.log2_page) - 1;
+    // whether any row sees one of the 16 keys from `k` on (pages that none does are not looked up)
+    auto group_seen = [&](int k) {
+      return k <= p_last && (A.window == 0 || k + 15 > (p_first > 0 ? p_first : 0) - A.window || k < A.sinks);
+    };
+    auto pages_of = [&](int j) {   // lane g: the page of the tile's keys 16 g ..
+      int b = -1;
+      if (j < nt && lane < kTileKeys / 16) {
+        const int k = all.key(j0 + j) + 16 * lane;
+        if (group_seen(k)) b = load_page(c, seq, k >> c.log2_page);
+      }
+      return b;
+    };
+    auto load = [&](int j, int kv, int pages, uint4 (&v)[kUnits]) {
+      const int key = j < nt ? all.key(j0 + j) : 0;
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const int kb = kb0 + kWays * i, b = __shfl_sync(0xffffffffu, pages, kb >> 1);
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (b >= 0) {
+          const size_t at = ((((size_t)b * c.kv_heads + head) << c.log2_page) + ((key + 8 * kb) & P1) + kr) * D;
+          v[i] = __ldg(reinterpret_cast<const uint4*>(c.codes[kv] + at + 64 * sub + 16 * col));
+        }
+      }
+    };
+    auto store = [&](uint8_t* dst, const uint4 (&v)[kUnits]) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        uint8_t* p = dst + sub * L::kHalf + (8 * (kb0 + kWays * i) + kr) * 128;
+        uint4 lo, hi;
+        widen4(v[i].x, lo.x, lo.y);
+        widen4(v[i].y, lo.z, lo.w);
+        widen4(v[i].z, hi.x, hi.y);
+        widen4(v[i].w, hi.z, hi.w);
+        *reinterpret_cast<uint4*>(p + (((2 * col) ^ kr) << 4)) = lo;
+        *reinterpret_cast<uint4*>(p + (((2 * col + 1) ^ kr) << 4)) = hi;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    uint4 kreg[kUnits], vreg[kUnits];
+    int pages = pages_of(0), next = -1;
+    load(0, 0, pages, kreg);
+    for (int j = 0; j < nt; ++j) {
+      const int st = j % kPreStages, par = (j / kPreStages + 1) & 1;
+      next = pages_of(j + 1);
+      float sk = 0.f, sv = 0.f;
+      if (w == 0 && lane < kTileKeys / 16 && pages >= 0) {
+        sk = __ldg(c.scales[0] + (size_t)pages * c.kv_heads + head);
+        sv = __ldg(c.scales[1] + (size_t)pages * c.kv_heads + head);
+      }
+      load(j, 1, pages, vreg);
+      if (!mbar_wait_warp(&S.kempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
+      if (w == 0 && lane < kTileKeys / 16) {
+        const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
+        // a > 0, so that a masked S = -inf gives x = -inf; a page that is not there has b = -inf
+        S.meta[j % kMeta][lane] = {fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f),
+                                   pages >= 0 ? __log2f(s) : -INFINITY, __frcp_rn(s), 0.f};
+      }
+      store(sm + L::kK + st * L::kTile, kreg);
+      if (lane == 0) mbar_arrive(&S.kfull[st]);
+      load(j + 1, 0, next, kreg);
+      if (!mbar_wait_warp(&S.vempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
+      store(sm + L::kV + st * L::kTile, vreg);
+      if (lane == 0) mbar_arrive(&S.vfull[st]);
+      pages = next;
+    }
+  } else {
+    reg_less<40>();
+    if (warp == 12 && nt > 0) {
+      // ------------------------------------------------------------------ MMAs
+      constexpr uint32_t kIdS = idesc_f16(kTileKeys, false), kIdO = idesc_f16(D, true);
+      const bool leader = elect_one();
+      auto wait = [&](uint64_t* bar, int par, int code) {
+        const bool ok = mbar_wait_warp(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
+        tc_fence_after();
+        return ok;
+      };
+      auto mma_s = [&](int t, int st) {
+        const uint32_t qa = smem_u32(sm + L::kQ + t * L::kTile), kb = smem_u32(sm + L::kK + st * L::kTile);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * L::kHalf + (k & 3) * 32;
+          mma_f16(tm + t * 128, sdesc_sw128(qa + off), sdesc_sw128(kb + off), kIdS, k > 0);
+        }
+      };
+      auto mma_o = [&](int t, int st, bool first) {
+        const uint32_t vb = smem_u32(sm + L::kV + st * L::kTile);
+#pragma unroll
+        for (int k = 0; k < kTileKeys / 16; ++k)
+          mma_f16_ts(tm + 256 + t * 128, tm + t * 128 + 8 * k, sdesc_mn128(vb + 2048 * k, L::kHalf), kIdO,
+                     !first || k > 0);
+      };
+      bool ok = wait(&S.kfull[0], 0, kDevTimeoutConv);
+      for (int t = 0; t < halves && ok; ++t) {
+        ok = wait(&S.qfull[t], 0, kDevTimeoutFull);
+        if (ok && leader) {
+          mma_s(t, 0);
+          mma_commit(&S.sfull[t]);
+          if (t == halves - 1) mma_commit(&S.kempty[0]);
+        }
+        __syncwarp();
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int st = j % kPreStages, s1 = (j + 1) % kPreStages;
+        const bool more = j + 1 < nt;
+        ok = wait(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
+        if (ok && more) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
+        for (int t = 0; t < halves && ok; ++t) {
+          ok = wait(&S.pfull[t], j, kDevTimeoutTmemEmpty);
+          if (ok && leader) {
+            mma_o(t, st, j == 0);
+            if (more) {
+              mma_s(t, s1);
+              mma_commit(&S.sfull[t]);
+            } else {
+              mma_commit(&S.ofull[t]);
+            }
+            if (t == halves - 1) {
+              mma_commit(&S.vempty[st]);
+              if (more) mma_commit(&S.kempty[s1]);
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok) {   // a wait gave up: the MMAs under way end before tensor memory is freed
+        if (leader) mma_commit(&S.drain);
+        __syncwarp();
+        int no_abort = 0;
+        mbar_wait_warp(&S.drain, 0, &no_abort, c.err, kDevTimeoutDrain, A.wait_cycles);
+      }
+    }
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 12) {
+    tmem_relinquish<false>();
+    tmem_dealloc<false>(tm, 512);
+  }
+}
+
+// Joins the parts of the keys: a warp a row.
+template <int D>
+__global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, int nsplit, int tiles) {
+  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, head = blockIdx.y, seq = blockIdx.z;
+  Seq q;
+  if (!load_seq(A.c, seq, q, false) || row >= q.n * A.group) return;
+  const int tile = row / (2 * kTileRows), r = row % (2 * kTileRows);
+  constexpr size_t kPart = 2 * kTileRows * (D + 2);
+  const float* part = A.ws + (((size_t)seq * tiles + tile) * gridDim.y + head) * nsplit * kPart;
+  float M = -INFINITY;
+  for (int i = lane; i < nsplit; i += 32) M = fmaxf(M, __ldg(part + i * kPart + 2 * kTileRows * D + r));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  const float base = M == -INFINITY ? 0.f : M;
+  constexpr int E = D / 32;
+  float l = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < nsplit; ++i) {
+    const float* p = part + i * kPart;
+    const float f = exp2_fast(__ldg(p + 2 * kTileRows * D + r) - base);
+    l = fmaf(f, __ldg(p + 2 * kTileRows * (D + 1) + r), l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldg(p + (size_t)r * D + E * lane + e), o[e]);
+  }
+  const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+  const int tok = row / A.group, hh = row - tok * A.group;
+  __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; e += 2) *reinterpret_cast<__half2*>(dst + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
+}
+
+template <int D>
+static cudaError_t launch_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {
+  const int tiles = ceil_div((long long)a.c.max_tokens * a.group, 2 * kTileRows);
+  const long long ctas = (long long)tiles * a.c.kv_heads * a.c.seqs;
+  if (tiles > 65535) return cudaErrorInvalidValue;
+  // Grids that leave half of the SMs without a CTA are split along the keys, but not below
+  // two tiles of 128 keys a CTA.
+  const long long key_tiles = ceil_div(a.window > 0 && a.window + a.sinks < a.c.max_len - a.c.max_tokens
+                                           ? (long long)a.window + a.sinks + a.c.max_tokens
+                                           : a.c.max_len,
+                                       kTileKeys);
+  long long nsplit = num_sms / ctas;
+  if (nsplit > key_tiles / 2) nsplit = key_tiles / 2;
+  constexpr int smem = PreLayout<D>::kBytes;
+  const auto fn = nsplit > 1 ? kv8_prefill_kernel<D, true> : kv8_prefill_kernel<D, false>;
+  const cudaError_t e = ensure_max_dyn_smem(fn);
+  if (e != cudaSuccess) return e;
+  if (nsplit <= 1) {
+    fn<<<dim3(a.c.kv_heads, a.c.seqs, tiles), kPreThreads, smem, s>>>(a, 1);
+    return cudaGetLastError();
+  }
+  fn<<<dim3(a.c.kv_heads, a.c.seqs, (unsigned)(tiles * nsplit)), kPreThreads, smem, s>>>(a, (int)nsplit);
+  const cudaError_t e2 = cudaGetLastError();
+  if (e2 != cudaSuccess) return e2;
+  const int rows = a.c.max_tokens * a.group;
+  kv8_join_kernel<D><<<dim3(ceil_div(rows, 8), a.c.kv_heads, a.c.seqs), 256, 0, s>>>(a, (int)nsplit, tiles);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv8_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {
+  return a.c.head_dim == 64 ? launch_prefill<64>(a, num_sms, s) : launch_prefill<128>(a, num_sms, s);
+}
+
+}  // namespace dptq
