@@ -27,6 +27,7 @@
 namespace dptq {
 
 constexpr int kPreThreads = 512, kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
+constexpr int kNoEntry = (int)0x80000000;
 
 struct KeyMeta {     // of 16 keys
   float a, b, inv;   // x = a S + b; 1 / sv
@@ -309,25 +310,31 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     auto group_seen = [&](int k) {
       return k <= p_last && (A.window == 0 || k + 15 > (p_first > 0 ? p_first : 0) - A.window || k < A.sinks);
     };
-    auto pages_of = [&](int j) {   // lane g: the page of the tile's keys 16 g ..
-      int b = -1;
-      if (j < nt && lane < kTileKeys / 16) {
-        const int k = all.key(j0 + j) + 16 * lane;
-        if (group_seen(k)) b = load_page(c, seq, k >> c.log2_page);
-      }
-      return b;
+    // Lane g: the table's entry for the tile's keys 16 g .. (-1: not needed), asked for two tiles
+    // ahead; it is checked when it has come.
+    auto entry_of = [&](int j) {
+      const int k = (j < nt ? all.key(j0 + j) : 0) + 16 * lane;
+      const bool on = j < nt && lane < kTileKeys / 16 && group_seen(k);
+      return on ? __ldg(c.table + (long long)seq * c.table_stride + (k >> c.log2_page)) : kNoEntry;
     };
+    auto checked = [&](int b) {
+      if (b == kNoEntry) return -1;
+      if (b >= 0 && b < c.num_blocks) return b;
+      atomicCAS(c.err, 0, kDevBadPage);
+      return -1;
+    };
+    // (a page that is not there reads page 0: its keys have b = -inf below, and any codes do)
     auto load = [&](int j, int kv, int pages, uint4 (&v)[kUnits]) {
-      const int key = j < nt ? all.key(j0 + j) : 0;
+      const int key = all.key(j0 + j);
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int kb = kb0 + kWays * i, b = __shfl_sync(0xffffffffu, pages, kb >> 1);
-        v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (b >= 0) {
-          const size_t at = ((((size_t)b * c.kv_heads + head) << c.log2_page) + ((key + 8 * kb) & P1) + kr) * D;
-          v[i] = __ldg(reinterpret_cast<const uint4*>(c.codes[kv] + at + 64 * sub + 16 * col));
-        }
+        const int kb = kb0 + kWays * i, b = max(__shfl_sync(0xffffffffu, pages, kb >> 1), 0);
+        const size_t at = ((((size_t)b * c.kv_heads + head) << c.log2_page) + ((key + 8 * kb) & P1) + kr) * D;
+        v[i] = __ldg(reinterpret_cast<const uint4*>(c.codes[kv] + at + 64 * sub + 16 * col));
       }
+    };
+    auto scale_of = [&](int kv, int pages) {   // (written to the tile's KeyMeta by one warp)
+      return w == 0 && pages >= 0 ? __ldg(c.scales[kv] + (size_t)pages * c.kv_heads + head) : 0.f;
     };
     auto store = [&](uint8_t* dst, const uint4 (&v)[kUnits]) {
 #pragma unroll
@@ -345,31 +352,31 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       __syncwarp();
     };
     uint4 kreg[kUnits], vreg[kUnits];
-    int pages = pages_of(0), next = -1;
-    load(0, 0, pages, kreg);
+    int pages = checked(entry_of(0)), entry = entry_of(1);
+    float sk = scale_of(0, pages), sv = scale_of(1, pages);
+    if (nt > 0) load(0, 0, pages, kreg);
     for (int j = 0; j < nt; ++j) {
       const int st = j % kPreStages, par = (j / kPreStages + 1) & 1;
-      next = pages_of(j + 1);
-      float sk = 0.f, sv = 0.f;
-      if (w == 0 && lane < kTileKeys / 16 && pages >= 0) {
-        sk = __ldg(c.scales[0] + (size_t)pages * c.kv_heads + head);
-        sv = __ldg(c.scales[1] + (size_t)pages * c.kv_heads + head);
-      }
+      const int next = checked(entry);
+      entry = entry_of(j + 2);
       load(j, 1, pages, vreg);
+      const float sk1 = scale_of(0, next), sv1 = scale_of(1, next);
       if (!mbar_wait_warp(&S.kempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
       if (w == 0 && lane < kTileKeys / 16) {
         const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-        // a > 0, so that a masked S = -inf gives x = -inf; a page that is not there has b = -inf
+        // a > 0, so that a masked S = -inf gives x = -inf
         S.meta[j % kMeta][lane] = {fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f),
                                    pages >= 0 ? __log2f(s) : -INFINITY, __frcp_rn(s), 0.f};
       }
       store(sm + L::kK + st * L::kTile, kreg);
       if (lane == 0) mbar_arrive(&S.kfull[st]);
-      load(j + 1, 0, next, kreg);
+      if (j + 1 < nt) load(j + 1, 0, next, kreg);
       if (!mbar_wait_warp(&S.vempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
       store(sm + L::kV + st * L::kTile, vreg);
       if (lane == 0) mbar_arrive(&S.vfull[st]);
       pages = next;
+      sk = sk1;
+      sv = sv1;
     }
   } else {
     reg_less<40>();
