@@ -36,7 +36,7 @@ struct KeyMeta {     // of 16 keys
 struct PreShared {
   KeyMeta meta[kMeta][kTileKeys / 16];
   uint64_t kfull[kPreStages], kempty[kPreStages], vfull[kPreStages], vempty[kPreStages];
-  uint64_t qfull[2], sfull[2], pfull[2], ofull[2], drain;
+  uint64_t qfull[2], sfull[2], pfull[2][2], ofull[2], drain;   // pfull: halves of a tile's keys
   uint32_t tmem;
   int abort;
 };
@@ -78,6 +78,11 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
         "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
         "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(taddr));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 template <int N>
 __device__ __forceinline__ void reg_more() {
@@ -147,7 +152,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(&S.qfull[t], kTileRows);
-      mbar_init(&S.pfull[t], kTileRows);
+      mbar_init(&S.pfull[t][0], kTileRows);
+      mbar_init(&S.pfull[t][1], kTileRows);
       mbar_init(&S.sfull[t], 1);
       mbar_init(&S.ofull[t], 1);
     }
@@ -164,7 +170,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax, a row a thread
-    reg_more<184>();
+    reg_more<160>();
     const int t = warp >> 2, r = tid & (kTileRows - 1), row = row0 + t * kTileRows + r;
     const bool mine = row < row0 + nrows;
     const int tok = row / A.group, hh = row - tok * A.group;
@@ -194,66 +200,79 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         ok = mbar_wait_warp(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
         if (!ok) break;
         tc_fence_after();
-        float x[kTileKeys];
-#pragma unroll
-        for (int k = 0; k < kTileKeys; k += 32) tmem_ld32(tS + k, x + k);
-        tmem_ld_wait();
         const int key = all.key(j0 + j);
         const bool seen = key + kTileKeys - 1 <= p_lo &&
                           (A.window == 0 || key > p_hi - A.window || key + kTileKeys <= A.sinks);
-        if (!seen) {
-#pragma unroll
-          for (int k = 0; k < kTileKeys; ++k)
-            if (!kv8_sees(pos, key + k, A.window, A.sinks)) x[k] = -INFINITY;
-        }
         const KeyMeta* meta = S.meta[j % kMeta];
+        // S comes in halves of 64 keys, the first one twice: once for the maximum, once for the weights
+        float x[64];
+        auto load_half = [&](int h) {
+          tmem_ld32(tS + 64 * h, x);
+          tmem_ld32(tS + 64 * h + 32, x + 32);
+          tmem_ld_wait();
+          if (!seen) {
+#pragma unroll
+            for (int k = 0; k < 64; ++k)
+              if (!kv8_sees(pos, key + 64 * h + k, A.window, A.sinks)) x[k] = -INFINITY;
+          }
+        };
         float top = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < kTileKeys / 16; ++g) {
-          float v = x[16 * g];
+        for (int h = 0; h < 2; ++h) {
+          load_half(h);
 #pragma unroll
-          for (int k = 1; k < 16; ++k) v = fmaxf(v, x[16 * g + k]);
-          top = fmaxf(top, fmaf(v, meta[g].a, meta[g].b));
+          for (int g = 0; g < 4; ++g) {
+            float v[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k) v[k] = max3(x[16 * g + 3 * k], x[16 * g + 3 * k + 1], x[16 * g + 3 * k + 2]);
+            const float u = fmaxf(max3(v[0], v[1], v[2]), max3(v[3], v[4], x[16 * g + 15]));
+            top = fmaxf(top, fmaf(u, meta[4 * h + g].a, meta[4 * h + g].b));
+          }
         }
         if (__any_sync(0xffffffffu, top > m + 8.f)) {   // (m = -inf: the row's first keys)
           const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);
           m = mn;
           l *= f;
           if (j > 0) {   // (PV of tile j - 1 came before S of tile j, which is here)
-#pragma unroll
-            for (int k = 0; k < D; k += 32) {
-              float o[32];
-              tmem_ld32(tO + k, o);
+#pragma unroll 1
+            for (int k = 0; k < D; k += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO + k, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] *= f;
-              tmem_st32(tO + k, reinterpret_cast<const uint32_t(&)[32]>(o));
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st16(tO + k, o);
             }
           }
         }
         const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 1; h >= 0; --h) {   // 64 keys at a time: their product can begin
+          if (h == 0) load_half(0);
           uint32_t p[32];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const KeyMeta& mt = meta[4 * h + g];
-            const float a = mt.a, b = mt.b - base;
-            float sum = 0.f;
+            const uint64_t a = f2_pack(mt.a, mt.a), b = f2_pack(mt.b - base, mt.b - base);
+            uint64_t sum = 0;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
-              const float p0 = exp2_fast(fmaf(x[64 * h + 16 * g + k], a, b));
-              const float p1 = exp2_fast(fmaf(x[64 * h + 16 * g + k + 1], a, b));
-              sum += p0 + p1;
+              float p0, p1;
+              f2_unpack(f2_fma(f2_pack(x[16 * g + k], x[16 * g + k + 1]), a, b), p0, p1);
+              p0 = exp2_fast(p0);
+              p1 = exp2_fast(p1);
+              sum = k ? f2_add(sum, f2_pack(p0, p1)) : f2_pack(p0, p1);
               p[8 * g + k / 2] = pack_half2(p0, p1);
             }
-            l = fmaf(sum, mt.inv, l);
+            float s0, s1;
+            f2_unpack(sum, s0, s1);
+            l = fmaf(s0 + s1, mt.inv, l);
           }
-          tmem_st32(tS + 32 * h, p);
+          tmem_st32(tS + 64 + 32 * h, p);   // over the second half of S, which has been read
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&S.pfull[t][h]);
         }
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(&S.pfull[t]);
       }
       if (ok) ok = mbar_wait_warp(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
@@ -300,7 +319,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     tc_fence_before();
   } else if (warp < 12) {
     // ------------------------------------------------------------------ K and V, widened
-    reg_less<104>();
+    reg_less<112>();
     const int w = warp - 8, sub = D == 128 ? w & 1 : 0, kr = lane >> 2, col = lane & 3;
     constexpr int kWays = D == 128 ? 2 : 4;              // 8-key blocks side by side
     constexpr int kUnits = 16 / kWays;                   // blocks of a warp: 8 or 4
@@ -379,7 +398,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       sv = sv1;
     }
   } else {
-    reg_less<40>();
+    reg_less<80>();
     if (warp == 12 && nt > 0) {
       // ------------------------------------------------------------------ MMAs
       constexpr uint32_t kIdS = idesc_f16(kTileKeys, false), kIdO = idesc_f16(D, true);
@@ -397,12 +416,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           mma_f16(tm + t * 128, sdesc_sw128(qa + off), sdesc_sw128(kb + off), kIdS, k > 0);
         }
       };
-      auto mma_o = [&](int t, int st, bool first) {
+      auto mma_o = [&](int t, int st, int half, bool first) {   // (the second half of the keys comes first)
         const uint32_t vb = smem_u32(sm + L::kV + st * L::kTile);
 #pragma unroll
-        for (int k = 0; k < kTileKeys / 16; ++k)
-          mma_f16_ts(tm + 256 + t * 128, tm + t * 128 + 8 * k, sdesc_mn128(vb + 2048 * k, L::kHalf), kIdO,
-                     !first || k > 0);
+        for (int k = 4 * half; k < 4 * half + 4; ++k)
+          mma_f16_ts(tm + 256 + t * 128, tm + t * 128 + 64 + 8 * k, sdesc_mn128(vb + 2048 * k, L::kHalf), kIdO,
+                     !first || k > 4 * half);
       };
       bool ok = wait(&S.kfull[0], 0, kDevTimeoutConv);
       for (int t = 0; t < halves && ok; ++t) {
@@ -420,9 +439,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         ok = wait(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
         if (ok && more) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
         for (int t = 0; t < halves && ok; ++t) {
-          ok = wait(&S.pfull[t], j, kDevTimeoutTmemEmpty);
+          ok = wait(&S.pfull[t][1], j, kDevTimeoutTmemEmpty);
+          if (ok && leader) mma_o(t, st, 1, j == 0);
+          __syncwarp();
+          if (ok) ok = wait(&S.pfull[t][0], j, kDevTimeoutTmemEmpty);
           if (ok && leader) {
-            mma_o(t, st, j == 0);
+            mma_o(t, st, 0, false);
             if (more) {
               mma_s(t, s1);
               mma_commit(&S.sfull[t]);
