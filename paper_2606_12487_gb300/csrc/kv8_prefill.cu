@@ -93,6 +93,22 @@ __device__ __forceinline__ void reg_less() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
+// mbar_wait_warp in few instructions (the bound counts polls, of 64 cycles and more each): the
+// roles' loops together have to stay in the instruction cache.  With everything unrolled the
+// MMA warp spent more time on fetching its code than on issuing it.
+__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                               int code, long long limit) {
+  for (long long polls = limit >> 6; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); --polls) {
+    __nanosleep(20);
+    if (__any_sync(0xffffffffu, *abort_flag != 0 || polls <= 0)) {
+      *abort_flag = 1;
+      atomicCAS(err, 0, code);
+      return false;
+    }
+  }
+  return true;
+}
+
 // The 128-key tiles that a CTA's rows see: `sink` tiles from key 0, then tiles from key `from`.
 struct Tiles {
   int sink, from, count;
@@ -110,6 +126,11 @@ __device__ __forceinline__ Tiles row_tiles(int p_lo, int p_hi, int window, int s
   }
   r.count = r.sink + (p_hi + 1 - r.from + kTileKeys - 1) / kTileKeys;
   return r;
+}
+
+// The n lowest bits (n of any size).
+__device__ __forceinline__ uint64_t low_bits(int n) {
+  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
 }
 
 template <int D>
@@ -197,27 +218,30 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       const int p_lo = q.start + (row0 + t * kTileRows) / A.group;
       const int last = t == halves - 1 ? nrows - 1 : kTileRows - 1, p_hi = q.start + (row0 + last) / A.group;
       for (int j = 0; j < nt && ok; ++j) {
-        ok = mbar_wait_warp(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+        ok = mbar_wait_near(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         const int key = all.key(j0 + j);
         const bool seen = key + kTileKeys - 1 <= p_lo &&
                           (A.window == 0 || key > p_hi - A.window || key + kTileKeys <= A.sinks);
         const KeyMeta* meta = S.meta[j % kMeta];
-        // S comes in halves of 64 keys, the first one twice: once for the maximum, once for the weights
+        // S comes in halves of 64 keys, twice: for the maximum, then for the weights
         float x[64];
         auto load_half = [&](int h) {
           tmem_ld32(tS + 64 * h, x);
           tmem_ld32(tS + 64 * h + 32, x + 32);
           tmem_ld_wait();
-          if (!seen) {
+          if (!seen) {   // bit k: this row sees key k of the half
+            const int k0 = key + 64 * h;
+            uint64_t bits = low_bits(pos - k0 + 1);
+            if (A.window > 0) bits &= ~low_bits(pos - A.window + 1 - k0) | low_bits(A.sinks - k0);
 #pragma unroll
             for (int k = 0; k < 64; ++k)
-              if (!kv8_sees(pos, key + 64 * h + k, A.window, A.sinks)) x[k] = -INFINITY;
+              if (!((k < 32 ? (uint32_t)bits : (uint32_t)(bits >> 32)) >> (k & 31) & 1u)) x[k] = -INFINITY;
           }
         };
         float top = -INFINITY;
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           load_half(h);
 #pragma unroll
@@ -246,9 +270,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           }
         }
         const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
+#pragma unroll 1
         for (int h = 1; h >= 0; --h) {   // 64 keys at a time: their product can begin
-          if (h == 0) load_half(0);
+          load_half(h);
           uint32_t p[32];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
@@ -274,7 +298,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           mbar_arrive(&S.pfull[t][h]);
         }
       }
-      if (ok) ok = mbar_wait_warp(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+      if (ok) ok = mbar_wait_near(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
     }
     // ---- output
@@ -370,32 +394,36 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       fence_proxy_async_smem();
       __syncwarp();
     };
-    uint4 kreg[kUnits], vreg[kUnits];
-    int pages = checked(entry_of(0)), entry = entry_of(1);
+    // Units in order K 0, V 0, K 1, V 1, ..., each loaded while the one before it is widened.
+    uint4 cur[kUnits], nxt[kUnits];
+    int pages = checked(entry_of(0)), next = checked(entry_of(1)), entry = entry_of(2);
     float sk = scale_of(0, pages), sv = scale_of(1, pages);
-    if (nt > 0) load(0, 0, pages, kreg);
-    for (int j = 0; j < nt; ++j) {
-      const int st = j % kPreStages, par = (j / kPreStages + 1) & 1;
-      const int next = checked(entry);
-      entry = entry_of(j + 2);
-      load(j, 1, pages, vreg);
-      const float sk1 = scale_of(0, next), sv1 = scale_of(1, next);
-      if (!mbar_wait_warp(&S.kempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
-      if (w == 0 && lane < kTileKeys / 16) {
-        const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-        // a > 0, so that a masked S = -inf gives x = -inf
-        S.meta[j % kMeta][lane] = {fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f),
-                                   pages >= 0 ? __log2f(s) : -INFINITY, __frcp_rn(s), 0.f};
+    if (nt > 0) load(0, 0, pages, nxt);
+#pragma unroll 1
+    for (int u = 0; u < 2 * nt; ++u) {
+      const int j = u >> 1, kv = u & 1, st = j % kPreStages, par = (j / kPreStages + 1) & 1;
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) cur[i] = nxt[i];
+      if (u + 1 < 2 * nt) load((u + 1) >> 1, kv ^ 1, kv ? next : pages, nxt);
+      if (!mbar_wait_near(kv ? &S.vempty[st] : &S.kempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles))
+        break;
+      if (kv == 0) {
+        if (w == 0 && lane < kTileKeys / 16) {
+          const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
+          // a > 0, so that a masked S = -inf gives x = -inf
+          S.meta[j % kMeta][lane] = {fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f),
+                                     pages >= 0 ? __log2f(s) : -INFINITY, __frcp_rn(s), 0.f};
+        }
+        sk = scale_of(0, next);
+        sv = scale_of(1, next);
       }
-      store(sm + L::kK + st * L::kTile, kreg);
-      if (lane == 0) mbar_arrive(&S.kfull[st]);
-      if (j + 1 < nt) load(j + 1, 0, next, kreg);
-      if (!mbar_wait_warp(&S.vempty[st], par, abort_flag, c.err, kDevTimeoutEmpty, A.wait_cycles)) break;
-      store(sm + L::kV + st * L::kTile, vreg);
-      if (lane == 0) mbar_arrive(&S.vfull[st]);
-      pages = next;
-      sk = sk1;
-      sv = sv1;
+      store(sm + (kv ? L::kV : L::kK) + st * L::kTile, cur);
+      if (lane == 0) mbar_arrive(kv ? &S.vfull[st] : &S.kfull[st]);
+      if (kv) {
+        pages = next;
+        next = checked(entry);
+        entry = entry_of(j + 3);
+      }
     }
   } else {
     reg_less<80>();
@@ -404,24 +432,25 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       constexpr uint32_t kIdS = idesc_f16(kTileKeys, false), kIdO = idesc_f16(D, true);
       const bool leader = elect_one();
       auto wait = [&](uint64_t* bar, int par, int code) {
-        const bool ok = mbar_wait_warp(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
+        const bool ok = mbar_wait_near(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
         tc_fence_after();
         return ok;
       };
+      const uint64_t q0 = sdesc_sw128(smem_u32(sm + L::kQ)), k0 = sdesc_sw128(smem_u32(sm + L::kK));
+      const uint64_t v0 = sdesc_mn128(smem_u32(sm + L::kV), L::kHalf);
       auto mma_s = [&](int t, int st) {
-        const uint32_t qa = smem_u32(sm + L::kQ + t * L::kTile), kb = smem_u32(sm + L::kK + st * L::kTile);
+#pragma unroll 1
+        for (int h = 0; h < D / 64; ++h) {
+          const uint64_t a = q0 + ((t * L::kTile + h * L::kHalf) >> 4), b = k0 + ((st * L::kTile + h * L::kHalf) >> 4);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k >> 2) * L::kHalf + (k & 3) * 32;
-          mma_f16(tm + t * 128, sdesc_sw128(qa + off), sdesc_sw128(kb + off), kIdS, k > 0);
+          for (int k = 0; k < 4; ++k) mma_f16(tm + t * 128, a + 2 * k, b + 2 * k, kIdS, h > 0 || k > 0);
         }
       };
       auto mma_o = [&](int t, int st, int half, bool first) {   // (the second half of the keys comes first)
-        const uint32_t vb = smem_u32(sm + L::kV + st * L::kTile);
+        const uint32_t a = tm + t * 128 + 64 + 32 * half;
+        const uint64_t b = v0 + ((st * L::kTile + 8192 * half) >> 4);
 #pragma unroll
-        for (int k = 4 * half; k < 4 * half + 4; ++k)
-          mma_f16_ts(tm + 256 + t * 128, tm + t * 128 + 64 + 8 * k, sdesc_mn128(vb + 2048 * k, L::kHalf), kIdO,
-                     !first || k > 4 * half);
+        for (int k = 0; k < 4; ++k) mma_f16_ts(tm + 256 + t * 128, a + 8 * k, b + 128 * k, kIdO, !first || k > 0);
       };
       bool ok = wait(&S.kfull[0], 0, kDevTimeoutConv);
       for (int t = 0; t < halves && ok; ++t) {
@@ -433,11 +462,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         }
         __syncwarp();
       }
+#pragma unroll 1
       for (int j = 0; j < nt && ok; ++j) {
         const int st = j % kPreStages, s1 = (j + 1) % kPreStages;
         const bool more = j + 1 < nt;
         ok = wait(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
         if (ok && more) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
+#pragma unroll 1
         for (int t = 0; t < halves && ok; ++t) {
           ok = wait(&S.pfull[t][1], j, kDevTimeoutTmemEmpty);
           if (ok && leader) mma_o(t, st, 1, j == 0);
