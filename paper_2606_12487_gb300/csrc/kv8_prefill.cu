@@ -26,7 +26,7 @@
 
 namespace dptq {
 
-constexpr int kPreThreads = 512, kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
+constexpr int kConvWarps = 4, kMmaWarp = 8 + kConvWarps, kPreThreads = 32 * (kMmaWarp + 4), kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
 constexpr int kNoEntry = (int)0x80000000;
 
 struct KeyMeta {     // of 16 keys
@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 
   if (tid == 0) {
     for (int i = 0; i < kPreStages; ++i) {
-      mbar_init(&S.kfull[i], 4);
-      mbar_init(&S.vfull[i], 4);
+      mbar_init(&S.kfull[i], kConvWarps);
+      mbar_init(&S.vfull[i], kConvWarps);
       mbar_init(&S.kempty[i], 1);
       mbar_init(&S.vempty[i], 1);
     }
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     S.abort = 0;
     fence_mbar_init();
   }
-  if (warp == 12) tmem_alloc<false>(&S.tmem, 512);
+  if (warp == kMmaWarp) tmem_alloc<false>(&S.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -225,9 +225,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         const bool seen = key + kTileKeys - 1 <= p_lo &&
                           (A.window == 0 || key > p_hi - A.window || key + kTileKeys <= A.sinks);
         const KeyMeta* meta = S.meta[j % kMeta];
-        // S comes in halves of 64 keys, twice: for the maximum, then for the weights
+        // Halves of 64 keys, the second one first.  The weights are relative to a maximum that may
+        // lag by 2^8 (binary16 holds them), so the first half's are made before the other half is
+        // looked at; where that one then raises the maximum, they are rescaled as O is.
         float x[64];
-        auto load_half = [&](int h) {
+        uint32_t p[32];
+#pragma unroll 1
+        for (int h = 1; h >= 0; --h) {
           tmem_ld32(tS + 64 * h, x);
           tmem_ld32(tS + 64 * h + 32, x + 32);
           tmem_ld_wait();
@@ -239,64 +243,70 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
             for (int k = 0; k < 64; ++k)
               if (!((k < 32 ? (uint32_t)bits : (uint32_t)(bits >> 32)) >> (k & 31) & 1u)) x[k] = -INFINITY;
           }
-        };
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          load_half(h);
+          const KeyMeta* mh = meta + 4 * h;
+          float top = -INFINITY;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             float v[5];
 #pragma unroll
             for (int k = 0; k < 5; ++k) v[k] = max3(x[16 * g + 3 * k], x[16 * g + 3 * k + 1], x[16 * g + 3 * k + 2]);
             const float u = fmaxf(max3(v[0], v[1], v[2]), max3(v[3], v[4], x[16 * g + 15]));
-            top = fmaxf(top, fmaf(u, meta[4 * h + g].a, meta[4 * h + g].b));
+            top = fmaxf(top, fmaf(u, mh[g].a, mh[g].b));
           }
-        }
-        if (__any_sync(0xffffffffu, top > m + 8.f)) {   // (m = -inf: the row's first keys)
-          const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);
-          m = mn;
-          l *= f;
-          if (j > 0) {   // (PV of tile j - 1 came before S of tile j, which is here)
+          if (__any_sync(0xffffffffu, top > m + 8.f)) {   // (m = -inf: the row's first keys)
+            const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);
+            m = mn;
+            l *= f;
+            if (j > 0) {   // (PV of tile j - 1 came before S of tile j, which is here)
 #pragma unroll 1
-            for (int k = 0; k < D; k += 16) {
-              uint32_t o[16];
-              tmem_ld16(tO + k, o);
-              tmem_ld_wait();
+              for (int k = 0; k < D; k += 16) {
+                uint32_t o[16];
+                tmem_ld16(tO + k, o);
+                tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st16(tO + k, o);
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st16(tO + k, o);
+              }
+            }
+            if (h == 0) {
+              const __half2 f2 = __float2half2_rn(f);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&p[e]), f2);
+                p[e] = *reinterpret_cast<const uint32_t*>(&y);
+              }
             }
           }
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 1
-        for (int h = 1; h >= 0; --h) {   // 64 keys at a time: their product can begin
-          load_half(h);
-          uint32_t p[32];
+          if (h == 0) {
+            tmem_st32(tS + 96, p);   // over the second half of S, which has been read
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(&S.pfull[t][1]);
+          }
+          const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const KeyMeta& mt = meta[4 * h + g];
-            const uint64_t a = f2_pack(mt.a, mt.a), b = f2_pack(mt.b - base, mt.b - base);
+            const float b0 = mh[g].b - base;
+            const uint64_t a = f2_pack(mh[g].a, mh[g].a), b = f2_pack(b0, b0);
             uint64_t sum = 0;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
-              float p0, p1;
-              f2_unpack(f2_fma(f2_pack(x[16 * g + k], x[16 * g + k + 1]), a, b), p0, p1);
-              p0 = exp2_fast(p0);
-              p1 = exp2_fast(p1);
-              sum = k ? f2_add(sum, f2_pack(p0, p1)) : f2_pack(p0, p1);
-              p[8 * g + k / 2] = pack_half2(p0, p1);
+              float y0, y1;
+              f2_unpack(f2_fma(f2_pack(x[16 * g + k], x[16 * g + k + 1]), a, b), y0, y1);
+              y0 = exp2_fast(y0);
+              y1 = exp2_fast(y1);
+              sum = k ? f2_add(sum, f2_pack(y0, y1)) : f2_pack(y0, y1);
+              p[8 * g + k / 2] = pack_half2(y0, y1);
             }
             float s0, s1;
             f2_unpack(sum, s0, s1);
-            l = fmaf(s0 + s1, mt.inv, l);
+            l = fmaf(s0 + s1, mh[g].inv, l);
           }
-          tmem_st32(tS + 64 + 32 * h, p);   // over the second half of S, which has been read
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive(&S.pfull[t][h]);
         }
+        tmem_st32(tS + 64, p);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&S.pfull[t][0]);
       }
       if (ok) ok = mbar_wait_near(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
@@ -341,12 +351,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       }
     }
     tc_fence_before();
-  } else if (warp < 12) {
+  } else if (warp < kMmaWarp) {
     // ------------------------------------------------------------------ K and V, widened
     reg_less<112>();
     const int w = warp - 8, sub = D == 128 ? w & 1 : 0, kr = lane >> 2, col = lane & 3;
-    constexpr int kWays = D == 128 ? 2 : 4;              // 8-key blocks side by side
-    constexpr int kUnits = 16 / kWays;                   // blocks of a warp: 8 or 4
+    constexpr int kWays = D == 128 ? kConvWarps / 2 : kConvWarps;   // 8-key blocks side by side
+    constexpr int kUnits = 16 / kWays;                              // blocks of a warp: 8 or 4
     const int kb0 = D == 128 ? w >> 1 : w;
     const int P1 = (1 << c.log2_page) - 1;
     // whether any row sees one of the 16 keys from `k` on (pages that none does are not looked up)
@@ -427,7 +437,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     }
   } else {
     reg_less<80>();
-    if (warp == 12 && nt > 0) {
+    if (warp == kMmaWarp && nt > 0) {
       // ------------------------------------------------------------------ MMAs
       constexpr uint32_t kIdS = idesc_f16(kTileKeys, false), kIdO = idesc_f16(D, true);
       const bool leader = elect_one();
@@ -500,7 +510,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 12) {
+  if (warp == kMmaWarp) {
     tmem_relinquish<false>();
     tmem_dealloc<false>(tm, 512);
   }
