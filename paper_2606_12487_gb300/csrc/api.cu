@@ -905,13 +905,10 @@ dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16
     return fail(DPTQ_ERR_INVALID_ARG, "x, residual, gamma and residual_out must be 16-byte aligned");
   if ((reinterpret_cast<uintptr_t>(codes) & (bits == 8 ? 7u : 3u)) != 0 || (reinterpret_cast<uintptr_t>(scales) & 3u) != 0)
     return fail(DPTQ_ERR_INVALID_ARG, "codes must be aligned to 8 codes, scales to 4 bytes");
-  int dev;
-  dptq_status st = current_device(&dev);
-  if (st != DPTQ_OK) return st;
   NormArgs a{static_cast<const __half*>(x_fp16), static_cast<const __half*>(residual_fp16),
              static_cast<const __half*>(gamma_fp16), static_cast<__half*>(residual_out),
              static_cast<uint8_t*>(codes), scales, M, K, bits, eps};
-  DPTQ_CUDA(launch_norm_quant(a, 0, static_cast<cudaStream_t>(stream)), "norm_quant launch");
+  DPTQ_CUDA(launch_norm_quant(a, static_cast<cudaStream_t>(stream)), "norm_quant launch");
   return DPTQ_OK;
 }
 

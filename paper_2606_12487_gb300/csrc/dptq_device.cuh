@@ -400,6 +400,17 @@ __device__ __forceinline__ void tmem_ld_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// ------------------------------------------------------------------ quantizer
+// rint(x / s) of the IEEE quotient, ties to even, from x r with r = fl(1 / s) and |x / s| <= 128:
+// x r and the quotient differ by less than 2^-15 (two roundings of 2^-24), so only an x r that
+// close to a half needs the quotient.  s = 0 comes with r = 0; a NaN becomes 0 in the
+// conversion, and so does an infinite x, whose s is infinite.
+__device__ __forceinline__ int quant_code(float x, float s, float r) {
+  const float t = __fmul_rn(x, r), q = rintf(t);
+  if (fabsf(__fsub_rn(t, q)) >= 0.5f - 0x1p-15f) return __float2int_rn(__fdiv_rn(x, s));
+  return __float2int_rn(q);
+}
+
 // ------------------------------------------------------------------ packed fp32 pairs
 __device__ __forceinline__ uint64_t f2_pack(float a, float b) {
   uint64_t r;

@@ -114,7 +114,7 @@ struct NormArgs {
   int M, K, bits;
   float eps;
 };
-cudaError_t launch_norm_quant(const NormArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_norm_quant(const NormArgs& a, cudaStream_t s);
 
 // One call's view of a paged int8 cache and of the batch that it works on.
 struct Kv8Args {

@@ -43,12 +43,6 @@ __device__ __forceinline__ bool kv8_sees(int p, int j, int window, int sinks) {
   return j <= p && (window == 0 || j > p - window || j < sinks);
 }
 
-// rint(x / s) of the IEEE quotient, ties to even; 0 for a NaN quotient and for s = 0.
-// |x| <= 127 s but for the quotient's rounding, and an infinite x has an infinite s.
-__device__ __forceinline__ int quant_code(float x, float s) {
-  return s > 0.f ? __float2int_rn(__fdiv_rn(x, s)) : 0;
-}
-
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -120,6 +120,11 @@ def _stream(stream=None) -> int:
 
 
 def _check_tensor(t, dtype, shape, name):
+    try:   # (one pass over the attributes: 0.44 -> CHKUS us a tensor on a Grace core)
+        if t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+            return
+    except AttributeError:
+        pass
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
@@ -362,7 +367,7 @@ class Kv8Batch:
 def _check_heads(t, tokens, heads, dim, name):
     """float16 [tokens, heads, dim] with the heads of a token side by side; tokens any distance apart."""
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float16 or not t.is_cuda:
         raise TypeError(f"{name} must be a float16 CUDA tensor")
     if t.shape != (tokens, heads, dim):
         raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
