@@ -400,6 +400,14 @@ __device__ __forceinline__ void tmem_ld_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// ------------------------------------------------------------------ plain loads
+// Kernels that start while their predecessor ends (griddepcontrol.wait at their top) read what
+// it wrote: not with ld.global.nc (__ldg), whose data must not change while the kernel runs.
+template <class T>
+__device__ __forceinline__ T ld_plain(const T* p) {
+  return *p;
+}
+
 // ------------------------------------------------------------------ quantizer
 // rint(x / s) of the IEEE quotient, ties to even, from x r with r = fl(1 / s) and |x / s| <= 128:
 // x r and the quotient differ by less than 2^-15 (two roundings of 2^-24), so only an x r that

@@ -268,6 +268,34 @@ cudaError_t ensure_max_dyn_smem(Kernel* fn) {
   return ensure_max_dyn_smem_impl(reinterpret_cast<const void*>(fn));
 }
 
+// A launch that may begin while its predecessor on the stream ends (programmatic dependent
+// launch, unless DPTQ_PDL=0): the kernel waits (griddepcontrol.wait) before it touches memory.
+// cluster: CTAs of a cluster along x.
+template <class... Params, class... Args>
+cudaError_t launch_after(void (*fn)(Params...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, int cluster,
+                         Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (pdl_allowed()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)cluster;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = (unsigned)n;
+  return cudaLaunchKernelEx(&cfg, fn, static_cast<Params>(args)...);
+}
+
 // Message returned by dptq_last_error_message() on the calling thread.
 void set_error_message(const std::string& m);
 int gemm_pick_nt(int M, int bits, int KB);

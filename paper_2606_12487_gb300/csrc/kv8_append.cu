@@ -68,12 +68,14 @@ __global__ void __launch_bounds__(512, 3) kv8_append_pages_kernel(const Kv8Appen
   const Kv8Args& c = a.c;
   const int tid = threadIdx.x, kv = blockIdx.x & 1, head = blockIdx.x >> 1;
   const int vecs = c.head_dim / 8, log2v = c.head_dim == 64 ? 3 : 4;   // vectors of a row
+  pdl_launch_dependents();
+  pdl_wait();
   Seq q;
   if (!load_seq(c, blockIdx.z, q, tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) || q.len == 0 || q.n == 0) return;
   const int first = q.start > 0 ? q.start : 0, page = (first >> c.log2_page) + blockIdx.y;
   if (page << c.log2_page >= q.len) return;
   const PageRows pr = page_rows(q, first, page, c.log2_page);
-  const int entry = __ldg(c.table + (long long)blockIdx.z * c.table_stride + page);   // (looked at after the rows are asked for)
+  const int entry = ld_plain(c.table + (long long)blockIdx.z * c.table_stride + page);   // (looked at after the rows are asked for)
   const __half* src = (kv ? a.rows[1] : a.rows[0]) + (q.tok0 + pr.p0 - (long long)q.start) * a.stride +
                       (size_t)head * c.head_dim;
   uint4 x[kAppendVecs];
@@ -83,7 +85,7 @@ __global__ void __launch_bounds__(512, 3) kv8_append_pages_kernel(const Kv8Appen
     const int v = tid + i * blockDim.x, row = v >> log2v;
     x[i] = make_uint4(0u, 0u, 0u, 0u);
     if (row >= pr.lo && row < pr.hi)
-      x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * a.stride) + (v & (vecs - 1)));
+      x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (v & (vecs - 1)));
   }
   if (entry < 0 || entry >= c.num_blocks) {
     atomicCAS(c.err, 0, kDevBadPage);
@@ -118,6 +120,8 @@ __global__ void __launch_bounds__(256) kv8_append_few_kernel(const Kv8AppendArgs
   const int lane = threadIdx.x & 31, item = blockIdx.x * 8 + (threadIdx.x >> 5), kv = item & 1, head = item >> 1;
   const int vecs = c.head_dim / 8, log2v = c.head_dim == 64 ? 3 : 4;
   if (head >= c.kv_heads) return;
+  pdl_launch_dependents();
+  pdl_wait();
   Seq q;
   if (!load_seq(c, blockIdx.y, q, lane == 0 && item == 0) || q.len == 0 || q.n == 0) return;
   const int first = q.start > 0 ? q.start : 0, per = 32 >> log2v;   // rows side by side in the warp
@@ -138,7 +142,7 @@ __global__ void __launch_bounds__(256) kv8_append_few_kernel(const Kv8AppendArgs
     for (int i = 0; i < kRounds; ++i) {
       const int row = pr.lo + i * per + (lane >> log2v);
       x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < pr.hi) x[i] = __ldg(reinterpret_cast<const uint4*>(src + row * a.stride) + (lane & (vecs - 1)));
+      if (row < pr.hi) x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (lane & (vecs - 1)));
       am = abs_max8(x[i], am);
     }
 #pragma unroll
@@ -157,14 +161,11 @@ __global__ void __launch_bounds__(256) kv8_append_few_kernel(const Kv8AppendArgs
 }
 
 cudaError_t launch_kv8_append(const Kv8AppendArgs& a, cudaStream_t s) {
-  if (a.c.max_tokens <= kAppendFew) {
-    kv8_append_few_kernel<<<dim3(ceil_div(2 * a.c.kv_heads, 8), a.c.seqs), 256, 0, s>>>(a);
-  } else {
-    const int pages = ((a.c.max_tokens - 1) >> a.c.log2_page) + 2;
-    const int threads = (a.c.head_dim << a.c.log2_page) / (8 * kAppendVecs);   // 32 to 512
-    kv8_append_pages_kernel<<<dim3(2 * a.c.kv_heads, pages, a.c.seqs), threads, 0, s>>>(a);
-  }
-  return cudaGetLastError();
+  if (a.c.max_tokens <= kAppendFew)
+    return launch_after(kv8_append_few_kernel, dim3(ceil_div(2 * a.c.kv_heads, 8), a.c.seqs), 256, 0, s, 1, a);
+  const int pages = ((a.c.max_tokens - 1) >> a.c.log2_page) + 2;
+  const int threads = (a.c.head_dim << a.c.log2_page) / (8 * kAppendVecs);   // 32 to 512
+  return launch_after(kv8_append_pages_kernel, dim3(2 * a.c.kv_heads, pages, a.c.seqs), threads, 0, s, 1, a);
 }
 
 }  // namespace dptq

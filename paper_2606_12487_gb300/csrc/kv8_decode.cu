@@ -139,6 +139,9 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
   const int P = 1 << c.log2_page;
   Ring<D>& ring = rings[warp];
 
+  pdl_launch_dependents();
+  pdl_wait();
+
   // ---- this CTA's share
   long long total = 0;
   int some = 0;   // sequences with steps
@@ -209,7 +212,7 @@ __global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeC
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint2 v = make_uint2(0u, 0u);
-        if (row < rows) v = __ldg(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
+        if (row < rows) v = ld_plain(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
         qf[r][k][0] = v.x;
         qf[r][k][1] = v.y;
       }
@@ -544,8 +547,7 @@ static cudaError_t launch_decode(const Kv8AttendArgs& a, int num_sms, cudaStream
   if (e != cudaSuccess) return e;
   static_assert(kDecodeCtas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)
   if (num_sms > 256) return cudaErrorInvalidValue;
-  fn<<<num_sms * (RT == 1 ? kDecodeCtas8 : kDecodeCtas16), kDecThreads, smem, s>>>(a);
-  return cudaGetLastError();
+  return launch_after(fn, num_sms * (RT == 1 ? kDecodeCtas8 : kDecodeCtas16), kDecThreads, smem, s, 1, a);
 }
 
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {

@@ -19,7 +19,7 @@ struct Seq {
 // False (and, from the thread that `tells`, the error word) where the arrays contradict what
 // the call declared: such a sequence is left alone, so no index is made from its numbers.
 __device__ __forceinline__ bool load_seq(const Kv8Args& c, int s, Seq& q, bool tells) {
-  const int a = __ldg(c.cu + s), b = __ldg(c.cu + s + 1), len = __ldg(c.lens + s);
+  const int a = ld_plain(c.cu + s), b = ld_plain(c.cu + s + 1), len = ld_plain(c.lens + s);
   const bool ok = a >= 0 && b >= a && b <= c.tokens && b - a <= c.max_tokens && len >= 0 && len <= c.max_len;
   q.tok0 = a;
   q.n = b - a;
@@ -32,7 +32,7 @@ __device__ __forceinline__ bool load_seq(const Kv8Args& c, int s, Seq& q, bool t
 // The page that holds position p of sequence s, or -1 (and the error word) if the table has
 // none.  p < max_len <= table_stride * page, checked on the host and by load_seq.
 __device__ __forceinline__ int load_page(const Kv8Args& c, int s, int page) {
-  const int b = __ldg(c.table + (long long)s * c.table_stride + page);
+  const int b = ld_plain(c.table + (long long)s * c.table_stride + page);
   if (b >= 0 && b < c.num_blocks) return b;
   atomicCAS(c.err, 0, kDevBadPage);
   return -1;

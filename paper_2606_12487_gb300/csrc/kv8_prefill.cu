@@ -42,24 +42,41 @@ struct PreShared {
 };
 
 // D[tmem] (+)= A B^T, binary16 operands, fp32 accumulators: A in shared memory or tensor memory.
+// PAIR: 128 rows of A and D and half of B's columns in each CTA of a pair.
+template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
-// Instruction descriptor: binary16 operands, fp32 accumulators, 128 rows; b_mn: B's rows (N)
-// are contiguous instead of its K.
-__host__ __device__ constexpr uint32_t idesc_f16(int n, bool b_mn) {
-  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+// Instruction descriptor: binary16 operands, fp32 accumulators, m rows (128, or 256 of a pair);
+// b_mn: B's columns (N) are contiguous instead of its K.
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn) {
+  return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 // B with contiguous N in the 128-byte swizzle: atoms of 64 n x 8 k, 1024 bytes apart along k,
 // `n_stride` bytes apart along n.
@@ -133,32 +150,43 @@ __device__ __forceinline__ uint64_t low_bits(int n) {
   return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
 }
 
-template <int D>
+template <int D, bool PAIR>
 struct PreLayout {
-  static constexpr int kHalf = 128 * 128;               // 64 dims (or 64-dim group) x 128 rows
-  static constexpr int kTile = D / 64 * kHalf;          // a widened tile, or a row tile of q
-  static constexpr int kQ = 0, kK = 2 * kTile, kV = kK + kPreStages * kTile, kEnd = kV + kPreStages * kTile;
+  static constexpr int kHalf = 128 * 128;                          // 64 dims x 128 rows
+  static constexpr int kQTile = D / 64 * kHalf;                    // a row tile of q
+  static constexpr int kTile = PAIR ? kQTile / 2 : kQTile;         // this CTA's part of a widened tile:
+  static constexpr int kKHalf = PAIR ? kHalf / 2 : kHalf;          // K: 64 dims x its keys; V: its dims x 128 keys
+  static constexpr int kQ = 0, kK = 2 * kQTile, kV = kK + kPreStages * kTile, kEnd = kV + kPreStages * kTile;
   static constexpr int kBytes = kEnd + (int)sizeof(PreShared) + 1024;   // (1024: alignment)
 };
 
 // SPLIT: this CTA's part of the keys goes to the scratch, for kv8_join_kernel.
-template <int D, bool SPLIT>
+// PAIR: two CTAs of a cluster work on 512 rows, 256 each; the tensor cores of both take K and V
+// tiles of which each CTA widens and holds one half (of K's keys, of V's dims).  That halves the
+// widening, its stores and what the MMAs read of K and V from shared memory, which is what a
+// CTA alone is short of.  The first CTA issues the MMAs; the second one's widening and softmax
+// warps arrive on its barriers (mbar_arrive_remote says what that rests on).
+template <int D, bool SPLIT, bool PAIR>
 __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8AttendArgs A, int nsplit) {
-  using L = PreLayout<D>;
+  static_assert(!PAIR || (D == 128 && !SPLIT), "a pair's halves of V are 64 dims; few rows take no pairs");
+  using L = PreLayout<D, PAIR>;
+  constexpr int kCtas = PAIR ? 2 : 1, kRows = kCtas * 2 * kTileRows;   // rows of a CTA or pair
   extern __shared__ uint8_t raw[];
   uint8_t* sm = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   PreShared& S = *reinterpret_cast<PreShared*>(sm + L::kEnd);
   const Kv8Args& c = A.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int head = blockIdx.x, seq = blockIdx.y;
+  const int head = blockIdx.x / kCtas, rank = PAIR ? blockIdx.x & 1 : 0, seq = blockIdx.y;
   const int split = SPLIT ? blockIdx.z % nsplit : 0, zt = SPLIT ? blockIdx.z / nsplit : blockIdx.z;
+  pdl_launch_dependents();
+  pdl_wait();
   Seq q;
   if (!load_seq(c, seq, q, tid == 0 && blockIdx.z == 0 && head == 0)) return;
   const int rows = q.n * A.group;
-  const int tile = (rows + 2 * kTileRows - 1) / (2 * kTileRows) - 1 - zt;   // the last rows, with the most keys, first
+  const int tile = (rows + kRows - 1) / kRows - 1 - zt;   // the last rows, with the most keys, first
   if (tile < 0) return;
-  const int row0 = tile * 2 * kTileRows, nrows = rows - row0 < 2 * kTileRows ? rows - row0 : 2 * kTileRows;
-  const int halves = nrows > kTileRows ? 2 : 1;
+  const int row0 = tile * kRows, nrows = rows - row0 < kRows ? rows - row0 : kRows;
+  const int halves = nrows > kCtas * kTileRows ? 2 : 1;   // row tiles (of a pair: 256 rows)
   const int p_first = q.start + row0 / A.group, p_last = q.start + (row0 + nrows - 1) / A.group;
   const Tiles all = row_tiles(p_first, p_last, A.window, A.sinks);
   const int j0 = SPLIT ? (int)((long long)all.count * split / nsplit) : 0;
@@ -166,15 +194,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 
   if (tid == 0) {
     for (int i = 0; i < kPreStages; ++i) {
-      mbar_init(&S.kfull[i], kConvWarps);
-      mbar_init(&S.vfull[i], kConvWarps);
+      mbar_init(&S.kfull[i], kCtas * kConvWarps);
+      mbar_init(&S.vfull[i], kCtas * kConvWarps);
       mbar_init(&S.kempty[i], 1);
       mbar_init(&S.vempty[i], 1);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&S.qfull[t], kTileRows);
-      mbar_init(&S.pfull[t][0], kTileRows);
-      mbar_init(&S.pfull[t][1], kTileRows);
+      mbar_init(&S.qfull[t], kCtas * kTileRows / 32);
+      mbar_init(&S.pfull[t][0], kCtas * kTileRows / 32);
+      mbar_init(&S.pfull[t][1], kCtas * kTileRows / 32);
       mbar_init(&S.sfull[t], 1);
       mbar_init(&S.ofull[t], 1);
     }
@@ -182,17 +210,31 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     S.abort = 0;
     fence_mbar_init();
   }
-  if (warp == kMmaWarp) tmem_alloc<false>(&S.tmem, 512);
+  if (warp == kMmaWarp) tmem_alloc<PAIR>(&S.tmem, 512);
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) {   // the other CTA's barriers are initialized
+    cluster_arrive();
+    cluster_wait();
+  }
   tc_fence_after();
+  // Arrives on a barrier of the CTA that issues the MMAs, for this warp.
+  auto tell = [&](uint64_t* bar) {
+    __syncwarp();
+    if (lane == 0) {
+      if (PAIR && rank != 0)
+        mbar_arrive_remote(cluster_map(smem_u32(bar), 0));
+      else
+        mbar_arrive(bar);
+    }
+  };
   const uint32_t tm = S.tmem;   // S of the row tiles at columns 0 and 128, O at 256 and 384
   volatile int* abort_flag = &S.abort;
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax, a row a thread
     reg_more<160>();
-    const int t = warp >> 2, r = tid & (kTileRows - 1), row = row0 + t * kTileRows + r;
+    const int t = warp >> 2, r = tid & (kTileRows - 1), row = row0 + (t * kCtas + rank) * kTileRows + r;
     const bool mine = row < row0 + nrows;
     const int tok = row / A.group, hh = row - tok * A.group;
     const int pos = mine ? q.start + tok : -1;
@@ -204,19 +246,20 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       {   // this row of q, negated for a negative scale
         const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
         const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D;
-        uint8_t* dst = sm + L::kQ + t * L::kTile + r * 128;
+        uint8_t* dst = sm + L::kQ + t * L::kQTile + r * 128;
 #pragma unroll
         for (int ch = 0; ch < D / 8; ++ch) {
-          uint4 v = mine ? __ldg(reinterpret_cast<const uint4*>(src) + ch) : make_uint4(0u, 0u, 0u, 0u);
+          uint4 v = mine ? ld_plain(reinterpret_cast<const uint4*>(src) + ch) : make_uint4(0u, 0u, 0u, 0u);
           v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
           *reinterpret_cast<uint4*>(dst + (ch >> 3) * L::kHalf + (((ch & 7) ^ (r & 7)) << 4)) = v;
         }
         fence_proxy_async_smem();
-        mbar_arrive(&S.qfull[t]);
+        tell(&S.qfull[t]);
       }
       // positions of this row tile's rows
-      const int p_lo = q.start + (row0 + t * kTileRows) / A.group;
-      const int last = t == halves - 1 ? nrows - 1 : kTileRows - 1, p_hi = q.start + (row0 + last) / A.group;
+      const int r_lo = (t * kCtas + rank) * kTileRows;
+      const int r_hi = r_lo + kTileRows - 1 < nrows - 1 ? r_lo + kTileRows - 1 : nrows - 1;
+      const int p_lo = q.start + (row0 + r_lo) / A.group, p_hi = q.start + (row0 + r_hi) / A.group;
       for (int j = 0; j < nt && ok; ++j) {
         ok = mbar_wait_near(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
         if (!ok) break;
@@ -281,7 +324,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
             tmem_st32(tS + 96, p);   // over the second half of S, which has been read
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(&S.pfull[t][1]);
+            tell(&S.pfull[t][1]);
           }
           const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -306,7 +349,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         tmem_st32(tS + 64, p);
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&S.pfull[t][0]);
+        tell(&S.pfull[t][0]);
       }
       if (ok) ok = mbar_wait_near(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
@@ -354,10 +397,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
   } else if (warp < kMmaWarp) {
     // ------------------------------------------------------------------ K and V, widened
     reg_less<112>();
-    const int w = warp - 8, sub = D == 128 ? w & 1 : 0, kr = lane >> 2, col = lane & 3;
-    constexpr int kWays = D == 128 ? kConvWarps / 2 : kConvWarps;   // 8-key blocks side by side
-    constexpr int kUnits = 16 / kWays;                              // blocks of a warp: 8 or 4
-    const int kb0 = D == 128 ? w >> 1 : w;
+    const int w = warp - 8, kr = lane >> 2, col = lane & 3;
+    // A warp takes 64 dims of 8 keys at a time, kUnits times: blocks kb0 + kWays i of dims 64 sub ..;
+    // of a pair's tile, K: its 8 blocks of keys; V: its 64 dims.
+    constexpr int kUnits = (PAIR ? 8 : 16) * (D / 64) / kConvWarps;
+    constexpr int kWaysK = D == 128 ? kConvWarps / 2 : kConvWarps, kWaysV = PAIR ? kConvWarps : kWaysK;
+    const int subk = D == 128 ? w & 1 : 0, kbk = (PAIR ? 8 * rank : 0) + (D == 128 ? w >> 1 : w);
+    const int subv = PAIR ? rank : subk, kbv = PAIR ? w : kbk;
     const int P1 = (1 << c.log2_page) - 1;
     // whether any row sees one of the 16 keys from `k` on (pages that none does are not looked up)
     auto group_seen = [&](int k) {
@@ -368,7 +414,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     auto entry_of = [&](int j) {
       const int k = (j < nt ? all.key(j0 + j) : 0) + 16 * lane;
       const bool on = j < nt && lane < kTileKeys / 16 && group_seen(k);
-      return on ? __ldg(c.table + (long long)seq * c.table_stride + (k >> c.log2_page)) : kNoEntry;
+      return on ? ld_plain(c.table + (long long)seq * c.table_stride + (k >> c.log2_page)) : kNoEntry;
     };
     auto checked = [&](int b) {
       if (b == kNoEntry) return -1;
@@ -378,21 +424,25 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     };
     // (a page that is not there reads page 0: its keys have b = -inf below, and any codes do)
     auto load = [&](int j, int kv, int pages, uint4 (&v)[kUnits]) {
-      const int key = all.key(j0 + j);
+      const int key = all.key(j0 + j), kb0 = kv ? kbv : kbk, ways = kv ? kWaysV : kWaysK, sub = kv ? subv : subk;
+      const int8_t* codes = kv ? c.codes[1] : c.codes[0];
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int kb = kb0 + kWays * i, b = max(__shfl_sync(0xffffffffu, pages, kb >> 1), 0);
+        const int kb = kb0 + ways * i, b = max(__shfl_sync(0xffffffffu, pages, kb >> 1), 0);
         const size_t at = ((((size_t)b * c.kv_heads + head) << c.log2_page) + ((key + 8 * kb) & P1) + kr) * D;
-        v[i] = __ldg(reinterpret_cast<const uint4*>(c.codes[kv] + at + 64 * sub + 16 * col));
+        v[i] = ld_plain(reinterpret_cast<const uint4*>(codes + at + 64 * sub + 16 * col));
       }
     };
     auto scale_of = [&](int kv, int pages) {   // (written to the tile's KeyMeta by one warp)
-      return w == 0 && pages >= 0 ? __ldg(c.scales[kv] + (size_t)pages * c.kv_heads + head) : 0.f;
+      return w == 0 && pages >= 0 ? ld_plain((kv ? c.scales[1] : c.scales[0]) + (size_t)pages * c.kv_heads + head) : 0.f;
     };
-    auto store = [&](uint8_t* dst, const uint4 (&v)[kUnits]) {
+    auto store = [&](uint8_t* dst, int kv, const uint4 (&v)[kUnits]) {
+      dst += (kv ? (PAIR ? 0 : subv * L::kHalf) + 8 * kbv * 128 : subk * L::kKHalf + 8 * (kbk - (PAIR ? 8 * rank : 0)) * 128) +
+             kr * 128;
+      const int step = 8 * 128 * (kv ? kWaysV : kWaysK);
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        uint8_t* p = dst + sub * L::kHalf + (8 * (kb0 + kWays * i) + kr) * 128;
+        uint8_t* p = dst + step * i;
         uint4 lo, hi;
         widen4(v[i].x, lo.x, lo.y);
         widen4(v[i].y, lo.z, lo.w);
@@ -402,7 +452,6 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         *reinterpret_cast<uint4*>(p + (((2 * col + 1) ^ kr) << 4)) = hi;
       }
       fence_proxy_async_smem();
-      __syncwarp();
     };
     // Units in order K 0, V 0, K 1, V 1, ..., each loaded while the one before it is widened.
     uint4 cur[kUnits], nxt[kUnits];
@@ -427,8 +476,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         sk = scale_of(0, next);
         sv = scale_of(1, next);
       }
-      store(sm + (kv ? L::kV : L::kK) + st * L::kTile, cur);
-      if (lane == 0) mbar_arrive(kv ? &S.vfull[st] : &S.kfull[st]);
+      store(sm + (kv ? L::kV : L::kK) + st * L::kTile, kv, cur);
+      tell(kv ? &S.vfull[st] : &S.kfull[st]);
       if (kv) {
         pages = next;
         next = checked(entry);
@@ -437,9 +486,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     }
   } else {
     reg_less<80>();
-    if (warp == kMmaWarp && nt > 0) {
+    if (warp == kMmaWarp && nt > 0 && rank == 0) {
       // ------------------------------------------------------------------ MMAs
-      constexpr uint32_t kIdS = idesc_f16(kTileKeys, false), kIdO = idesc_f16(D, true);
+      constexpr uint32_t kIdS = idesc_f16(kCtas * kTileRows, kTileKeys, false), kIdO = idesc_f16(kCtas * kTileRows, D, true);
+      const auto commit = [](uint64_t* bar) { PAIR ? mma_commit_pair(bar) : mma_commit(bar); };   // (in both CTAs)
       const bool leader = elect_one();
       auto wait = [&](uint64_t* bar, int par, int code) {
         const bool ok = mbar_wait_near(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
@@ -451,24 +501,24 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       auto mma_s = [&](int t, int st) {
 #pragma unroll 1
         for (int h = 0; h < D / 64; ++h) {
-          const uint64_t a = q0 + ((t * L::kTile + h * L::kHalf) >> 4), b = k0 + ((st * L::kTile + h * L::kHalf) >> 4);
+          const uint64_t a = q0 + ((t * L::kQTile + h * L::kHalf) >> 4), b = k0 + ((st * L::kTile + h * L::kKHalf) >> 4);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mma_f16(tm + t * 128, a + 2 * k, b + 2 * k, kIdS, h > 0 || k > 0);
+          for (int k = 0; k < 4; ++k) mma_f16<PAIR>(tm + t * 128, a + 2 * k, b + 2 * k, kIdS, h > 0 || k > 0);
         }
       };
       auto mma_o = [&](int t, int st, int half, bool first) {   // (the second half of the keys comes first)
         const uint32_t a = tm + t * 128 + 64 + 32 * half;
         const uint64_t b = v0 + ((st * L::kTile + 8192 * half) >> 4);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_f16_ts(tm + 256 + t * 128, a + 8 * k, b + 128 * k, kIdO, !first || k > 0);
+        for (int k = 0; k < 4; ++k) mma_f16_ts<PAIR>(tm + 256 + t * 128, a + 8 * k, b + 128 * k, kIdO, !first || k > 0);
       };
       bool ok = wait(&S.kfull[0], 0, kDevTimeoutConv);
       for (int t = 0; t < halves && ok; ++t) {
         ok = wait(&S.qfull[t], 0, kDevTimeoutFull);
         if (ok && leader) {
           mma_s(t, 0);
-          mma_commit(&S.sfull[t]);
-          if (t == halves - 1) mma_commit(&S.kempty[0]);
+          commit(&S.sfull[t]);
+          if (t == halves - 1 && nt > kPreStages) commit(&S.kempty[0]);
         }
         __syncwarp();
       }
@@ -488,20 +538,21 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
             mma_o(t, st, 0, false);
             if (more) {
               mma_s(t, s1);
-              mma_commit(&S.sfull[t]);
+              commit(&S.sfull[t]);
             } else {
-              mma_commit(&S.ofull[t]);
+              commit(&S.ofull[t]);
             }
             if (t == halves - 1) {
-              mma_commit(&S.vempty[st]);
-              if (more) mma_commit(&S.kempty[s1]);
+              // (a slot that no tile follows in is waited for by nobody)
+              if (j + kPreStages < nt) commit(&S.vempty[st]);
+              if (j + 1 + kPreStages < nt) commit(&S.kempty[s1]);
             }
           }
           __syncwarp();
         }
       }
       if (!ok) {   // a wait gave up: the MMAs under way end before tensor memory is freed
-        if (leader) mma_commit(&S.drain);
+        if (leader) commit(&S.drain);
         __syncwarp();
         int no_abort = 0;
         mbar_wait_warp(&S.drain, 0, &no_abort, c.err, kDevTimeoutDrain, A.wait_cycles);
@@ -509,10 +560,14 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     }
   }
   __syncthreads();
+  if constexpr (PAIR) {   // neither CTA leaves, or frees what the other's MMAs read, before both are done
+    cluster_arrive();
+    cluster_wait();
+  }
   tc_fence_after();
   if (warp == kMmaWarp) {
-    tmem_relinquish<false>();
-    tmem_dealloc<false>(tm, 512);
+    tmem_relinquish<PAIR>();
+    tmem_dealloc<PAIR>(tm, 512);
   }
 }
 
@@ -520,13 +575,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 template <int D>
 __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, int nsplit, int tiles) {
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, head = blockIdx.y, seq = blockIdx.z;
+  pdl_launch_dependents();
+  pdl_wait();
   Seq q;
   if (!load_seq(A.c, seq, q, false) || row >= q.n * A.group) return;
   const int tile = row / (2 * kTileRows), r = row % (2 * kTileRows);
   constexpr size_t kPart = 2 * kTileRows * (D + 2);
   const float* part = A.ws + (((size_t)seq * tiles + tile) * gridDim.y + head) * nsplit * kPart;
   float M = -INFINITY;
-  for (int i = lane; i < nsplit; i += 32) M = fmaxf(M, __ldg(part + i * kPart + 2 * kTileRows * D + r));
+  for (int i = lane; i < nsplit; i += 32) M = fmaxf(M, __ldcg(part + i * kPart + 2 * kTileRows * D + r));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   const float base = M == -INFINITY ? 0.f : M;
@@ -537,10 +594,10 @@ __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, in
 #pragma unroll 4
   for (int i = 0; i < nsplit; ++i) {
     const float* p = part + i * kPart;
-    const float f = exp2_fast(__ldg(p + 2 * kTileRows * D + r) - base);
-    l = fmaf(f, __ldg(p + 2 * kTileRows * (D + 1) + r), l);
+    const float f = exp2_fast(__ldcg(p + 2 * kTileRows * D + r) - base);
+    l = fmaf(f, __ldcg(p + 2 * kTileRows * (D + 1) + r), l);
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldg(p + (size_t)r * D + E * lane + e), o[e]);
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldcg(p + (size_t)r * D + E * lane + e), o[e]);
   }
   const float inv = l == 0.f ? 0.f : __frcp_rn(l);
   const int tok = row / A.group, hh = row - tok * A.group;
@@ -548,6 +605,8 @@ __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, in
 #pragma unroll
   for (int e = 0; e < E; e += 2) *reinterpret_cast<__half2*>(dst + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
 }
+
+constexpr int kPairRows = 512;   // rows of a sequence and KV head from which pairs of CTAs take them
 
 template <int D>
 static cudaError_t launch_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {
@@ -562,20 +621,26 @@ static cudaError_t launch_prefill(const Kv8AttendArgs& a, int num_sms, cudaStrea
                                        kTileKeys);
   long long nsplit = num_sms / ctas;
   if (nsplit > key_tiles / 2) nsplit = key_tiles / 2;
-  constexpr int smem = PreLayout<D>::kBytes;
-  const auto fn = nsplit > 1 ? kv8_prefill_kernel<D, true> : kv8_prefill_kernel<D, false>;
+  if constexpr (D == 128) {
+    if (nsplit <= 1 && (long long)a.c.max_tokens * a.group >= kPairRows) {
+      const auto pair = kv8_prefill_kernel<D, false, true>;
+      const cudaError_t e = ensure_max_dyn_smem(pair);
+      if (e != cudaSuccess) return e;
+      const int tiles4 = ceil_div((long long)a.c.max_tokens * a.group, 4 * kTileRows);
+      return launch_after(pair, dim3(2 * a.c.kv_heads, a.c.seqs, tiles4), kPreThreads, PreLayout<D, true>::kBytes, s, 2, a, 1);
+    }
+  }
+  constexpr int smem = PreLayout<D, false>::kBytes;
+  const auto fn = nsplit > 1 ? kv8_prefill_kernel<D, true, false> : kv8_prefill_kernel<D, false, false>;
   const cudaError_t e = ensure_max_dyn_smem(fn);
   if (e != cudaSuccess) return e;
-  if (nsplit <= 1) {
-    fn<<<dim3(a.c.kv_heads, a.c.seqs, tiles), kPreThreads, smem, s>>>(a, 1);
-    return cudaGetLastError();
-  }
-  fn<<<dim3(a.c.kv_heads, a.c.seqs, (unsigned)(tiles * nsplit)), kPreThreads, smem, s>>>(a, (int)nsplit);
-  const cudaError_t e2 = cudaGetLastError();
+  if (nsplit <= 1) return launch_after(fn, dim3(a.c.kv_heads, a.c.seqs, tiles), kPreThreads, smem, s, 1, a, 1);
+  const cudaError_t e2 =
+      launch_after(fn, dim3(a.c.kv_heads, a.c.seqs, (unsigned)(tiles * nsplit)), kPreThreads, smem, s, 1, a, (int)nsplit);
   if (e2 != cudaSuccess) return e2;
   const int rows = a.c.max_tokens * a.group;
-  kv8_join_kernel<D><<<dim3(ceil_div(rows, 8), a.c.kv_heads, a.c.seqs), 256, 0, s>>>(a, (int)nsplit, tiles);
-  return cudaGetLastError();
+  return launch_after(kv8_join_kernel<D>, dim3(ceil_div(rows, 8), a.c.kv_heads, a.c.seqs), 256, 0, s, 1, a, (int)nsplit,
+                      tiles);
 }
 
 cudaError_t launch_kv8_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {

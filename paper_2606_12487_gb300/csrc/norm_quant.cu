@@ -113,6 +113,8 @@ __global__ void __launch_bounds__(kNormThreads, norm_ctas(V)) norm_quant_kernel(
   const int row = blockIdx.x;
   const size_t at = (size_t)row * a.K;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  pdl_launch_dependents();
+  pdl_wait();
   uint4 x[V], r[V];
   float sq = 0.f, am = 0.f;
 #pragma unroll
@@ -124,7 +126,7 @@ __global__ void __launch_bounds__(kNormThreads, norm_ctas(V)) norm_quant_kernel(
       if (a.residual) r[i] = *reinterpret_cast<const uint4*>(a.residual + at + k);
     }
   }
-  auto weight = [&](int k) { return a.gamma ? __ldg(reinterpret_cast<const uint4*>(a.gamma + k)) : zero; };
+  auto weight = [&](int k) { return a.gamma ? ld_plain(reinterpret_cast<const uint4*>(a.gamma + k)) : zero; };
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int k = 8 * (threadIdx.x + i * blockDim.x);
@@ -145,11 +147,13 @@ __global__ void __launch_bounds__(1024, 1) norm_quant_long_kernel(const NormArgs
   const int row = blockIdx.x;
   const size_t at = (size_t)row * a.K;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  pdl_launch_dependents();
+  pdl_wait();
   float sq = 0.f, am = 0.f;
   for (int k = 8 * threadIdx.x; k < a.K; k += 8 * blockDim.x) {
     const uint4 x = *reinterpret_cast<const uint4*>(a.x + at + k);
     const uint4 r = a.residual ? *reinterpret_cast<const uint4*>(a.residual + at + k) : zero;
-    const uint4 g = a.gamma ? __ldg(reinterpret_cast<const uint4*>(a.gamma + k)) : zero;
+    const uint4 g = a.gamma ? ld_plain(reinterpret_cast<const uint4*>(a.gamma + k)) : zero;
     norm_take(a, at, k, x, r, g, sq, am);
   }
   norm_reduce(sq, am, red);
@@ -159,21 +163,14 @@ __global__ void __launch_bounds__(1024, 1) norm_quant_long_kernel(const NormArgs
   const __half* h = a.residual ? a.residual_out : a.x;
   for (int k = 8 * threadIdx.x; k < a.K; k += 8 * blockDim.x)
     norm_put(a, at, k, *reinterpret_cast<const uint4*>(h + at + k),
-             a.gamma ? __ldg(reinterpret_cast<const uint4*>(a.gamma + k)) : zero, s, r);
+             a.gamma ? ld_plain(reinterpret_cast<const uint4*>(a.gamma + k)) : zero, s, r);
 }
 
 cudaError_t launch_norm_quant(const NormArgs& a, cudaStream_t s) {
   const int vecs = a.K / 8, v = ceil_div(vecs, kNormThreads);
   const int V = v == 3 ? 4 : v, threads = round_up(ceil_div(vecs, V), 32);
-  if (V == 1)
-    norm_quant_kernel<1><<<a.M, threads, 0, s>>>(a);
-  else if (V == 2)
-    norm_quant_kernel<2><<<a.M, threads, 0, s>>>(a);
-  else if (V == 4)
-    norm_quant_kernel<4><<<a.M, threads, 0, s>>>(a);
-  else
-    norm_quant_long_kernel<<<a.M, 1024, 0, s>>>(a);
-  return cudaGetLastError();
+  const auto fn = V == 1 ? norm_quant_kernel<1> : V == 2 ? norm_quant_kernel<2> : norm_quant_kernel<4>;
+  return V <= 4 ? launch_after(fn, a.M, threads, 0, s, 1, a) : launch_after(norm_quant_long_kernel, a.M, 1024, 0, s, 1, a);
 }
 
 }  // namespace dptq
