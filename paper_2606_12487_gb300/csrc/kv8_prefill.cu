@@ -36,7 +36,8 @@ struct KeyMeta {     // of 16 keys
 struct PreShared {
   KeyMeta meta[kMeta][kTileKeys / 16];
   uint64_t kfull[kPreStages], kempty[kPreStages], vfull[kPreStages], vempty[kPreStages];
-  uint64_t qfull[2], sfull[2], pfull[2][2], ofull[2], drain;   // pfull: halves of a tile's keys
+  uint64_t qfull[2], sfull[2], pfull[2][2], ofull[2], drain;   // pfull: the two halves of a tile's keys
+  uint64_t phalf[2];   // the first half's product is complete
   uint32_t tmem;
   int abort;
 };
@@ -96,6 +97,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* r) {
         "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
       : "r"(taddr));
 }
+// Waits for the tensor-memory loads under way; `r`'s values exist from here on.
+__device__ __forceinline__ void tmem_ld_arrived(float (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
+                 "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]),
+                 "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]),
+                 "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])::"memory");
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -146,8 +155,26 @@ __device__ __forceinline__ Tiles row_tiles(int p_lo, int p_hi, int window, int s
 }
 
 // The n lowest bits (n of any size).
-__device__ __forceinline__ uint64_t low_bits(int n) {
-  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
+}
+
+// Writes -inf over the scores of the keys that this thread's row does not see, in tensor memory: the
+// few tiles that need it pay for the pass, and the code that every tile runs stays short (with
+// the masks in its middle, 878 instead of MASKUS us for the 8192-token prompt).
+__device__ __forceinline__ void mask_scores(uint32_t tS, int pos, int key, int window, int sinks) {
+#pragma unroll 1
+  for (int k = 0; k < kTileKeys; k += 16) {
+    uint32_t v[16];
+    tmem_ld16(tS + k, v);
+    uint32_t bits = low_bits(pos - key - k + 1);   // bit e: the row sees key k + e
+    if (window > 0) bits &= ~low_bits(pos - window + 1 - key - k) | low_bits(sinks - key - k);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = bits >> e & 1u ? v[e] : 0xFF800000u;
+    tmem_st16(tS + k, v);
+  }
+  tmem_st_wait();
 }
 
 template <int D, bool PAIR>
@@ -204,6 +231,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       mbar_init(&S.pfull[t][0], kCtas * kTileRows / 32);
       mbar_init(&S.pfull[t][1], kCtas * kTileRows / 32);
       mbar_init(&S.sfull[t], 1);
+      mbar_init(&S.phalf[t], 1);
       mbar_init(&S.ofull[t], 1);
     }
     mbar_init(&S.drain, 1);
@@ -268,69 +296,22 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         const bool seen = key + kTileKeys - 1 <= p_lo &&
                           (A.window == 0 || key > p_hi - A.window || key + kTileKeys <= A.sinks);
         const KeyMeta* meta = S.meta[j % kMeta];
-        // Halves of 64 keys, the second one first.  The weights are relative to a maximum that may
-        // lag by 2^8 (binary16 holds them), so the first half's are made before the other half is
-        // looked at; where that one then raises the maximum, they are rescaled as O is.
-        float x[64];
+        if (!seen) mask_scores(tS, pos, key, A.window, A.sinks);
+        // Halves of 64 keys, the second one first: its weights take the place of its S, and their
+        // product begins while the first half is worked on.  The weights are relative to a maximum
+        // that may lag by 2^8 (binary16 holds them), so they are made before the half's own maximum
+        // is known; where that is larger still, what is relative to the old one is rescaled and
+        // the half made again.
+        float xa[32], xb[32];
         uint32_t p[32];
-#pragma unroll 1
-        for (int h = 1; h >= 0; --h) {
-          tmem_ld32(tS + 64 * h, x);
-          tmem_ld32(tS + 64 * h + 32, x + 32);
-          tmem_ld_wait();
-          if (!seen) {   // bit k: this row sees key k of the half
-            const int k0 = key + 64 * h;
-            uint64_t bits = low_bits(pos - k0 + 1);
-            if (A.window > 0) bits &= ~low_bits(pos - A.window + 1 - k0) | low_bits(A.sinks - k0);
-#pragma unroll
-            for (int k = 0; k < 64; ++k)
-              if (!((k < 32 ? (uint32_t)bits : (uint32_t)(bits >> 32)) >> (k & 31) & 1u)) x[k] = -INFINITY;
-          }
-          const KeyMeta* mh = meta + 4 * h;
-          float top = -INFINITY;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            float v[5];
-#pragma unroll
-            for (int k = 0; k < 5; ++k) v[k] = max3(x[16 * g + 3 * k], x[16 * g + 3 * k + 1], x[16 * g + 3 * k + 2]);
-            const float u = fmaxf(max3(v[0], v[1], v[2]), max3(v[3], v[4], x[16 * g + 15]));
-            top = fmaxf(top, fmaf(u, mh[g].a, mh[g].b));
-          }
-          if (__any_sync(0xffffffffu, top > m + 8.f)) {   // (m = -inf: the row's first keys)
-            const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);
-            m = mn;
-            l *= f;
-            if (j > 0) {   // (PV of tile j - 1 came before S of tile j, which is here)
-#pragma unroll 1
-              for (int k = 0; k < D; k += 16) {
-                uint32_t o[16];
-                tmem_ld16(tO + k, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                tmem_st16(tO + k, o);
-              }
-            }
-            if (h == 0) {
-              const __half2 f2 = __float2half2_rn(f);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&p[e]), f2);
-                p[e] = *reinterpret_cast<const uint32_t*>(&y);
-              }
-            }
-          }
-          if (h == 0) {
-            tmem_st32(tS + 96, p);   // over the second half of S, which has been read
-            tmem_st_wait();
-            tc_fence_before();
-            tell(&S.pfull[t][1]);
-          }
+        // A quarter's weights, packed, their sum, and its largest x: h its place in the tile.
+        auto quarter = [&](float (&x)[32], int h, uint32_t* w, float& s, float& top) {
+          const KeyMeta* mh = meta + 2 * h;
           const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float b0 = mh[g].b - base;
-            const uint64_t a = f2_pack(mh[g].a, mh[g].a), b = f2_pack(b0, b0);
+          for (int g = 0; g < 2; ++g) {
+            const float a0 = mh[g].a, b0 = mh[g].b;
+            const uint64_t a = f2_pack(a0, a0), b = f2_pack(b0 - base, b0 - base);
             uint64_t sum = 0;
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
@@ -339,17 +320,79 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
               y0 = exp2_fast(y0);
               y1 = exp2_fast(y1);
               sum = k ? f2_add(sum, f2_pack(y0, y1)) : f2_pack(y0, y1);
-              p[8 * g + k / 2] = pack_half2(y0, y1);
+              w[8 * g + k / 2] = pack_half2(y0, y1);
             }
             float s0, s1;
             f2_unpack(sum, s0, s1);
-            l = fmaf(s0 + s1, mh[g].inv, l);
+            s = fmaf(s0 + s1, mh[g].inv, s);
+            float v[5];
+#pragma unroll
+            for (int k = 0; k < 5; ++k) v[k] = max3(x[16 * g + 3 * k], x[16 * g + 3 * k + 1], x[16 * g + 3 * k + 2]);
+            const float u = fmaxf(max3(v[0], v[1], v[2]), max3(v[3], v[4], x[16 * g + 15]));
+            top = fmaxf(top, fmaf(u, a0, b0));
+          }
+        };
+        if (j == 0) {   // the first maximum, so that the first half is not made for nothing
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            tmem_ld32(tS + 32 * h, xa);
+            tmem_ld_arrived(xa);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              float v = xa[16 * g];
+#pragma unroll
+              for (int k = 1; k < 15; k += 2) v = max3(v, xa[16 * g + k], xa[16 * g + k + 1]);
+              m = fmaxf(m, fmaf(fmaxf(v, xa[16 * g + 15]), meta[2 * h + g].a, meta[2 * h + g].b));
+            }
           }
         }
-        tmem_st32(tS + 64, p);
-        tmem_st_wait();
-        tc_fence_before();
-        tell(&S.pfull[t][0]);
+        tmem_ld32(tS + 64, xa);
+        int n = 0;
+#pragma unroll 1
+        for (;;) {   // (once, but for maxima that grow: that code stands apart from what every tile runs)
+          float top;
+#pragma unroll 1
+          for (; n < 2; ++n) {
+            const int h = 2 - 2 * n;
+            float s = 0.f;
+            top = -INFINITY;
+            tmem_ld_arrived(xa);
+            tmem_ld32(tS + 32 * h + 32, xb);   // (under the first quarter's work)
+            quarter(xa, h, p, s, top);
+            tmem_ld_arrived(xb);
+            quarter(xb, h + 1, p + 16, s, top);
+            if (__any_sync(0xffffffffu, top > m + 8.f)) break;
+            l += s;
+            tmem_st32(tS + 64 + 32 * n, p);
+            if (n == 0) tmem_ld32(tS, xa);
+            tmem_st_wait();
+            tc_fence_before();
+            tell(&S.pfull[t][n]);
+          }
+          if (n == 2) break;
+          const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);   // (m = -inf: no key yet)
+          m = mn;
+          l *= f;
+          // O: PV of tile j - 1 came before S of tile j, which is here; of tile j, the first half's
+          // product may be under way.
+          if (n == 1) {
+            ok = mbar_wait_near(&S.phalf[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+            if (!ok) break;
+            tc_fence_after();
+          }
+          if (j > 0 || n == 1) {
+#pragma unroll 1
+            for (int k = 0; k < D; k += 16) {
+              uint32_t o[16];
+              tmem_ld16(tO + k, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st16(tO + k, o);
+            }
+          }
+          tmem_ld32(tS + 64 * (1 - n), xa);
+        }
       }
       if (ok) ok = mbar_wait_near(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
@@ -506,9 +549,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           for (int k = 0; k < 4; ++k) mma_f16<PAIR>(tm + t * 128, a + 2 * k, b + 2 * k, kIdS, h > 0 || k > 0);
         }
       };
-      auto mma_o = [&](int t, int st, int half, bool first) {   // (the second half of the keys comes first)
-        const uint32_t a = tm + t * 128 + 64 + 32 * half;
-        const uint64_t b = v0 + ((st * L::kTile + 8192 * half) >> 4);
+      auto mma_o = [&](int t, int st, int n, bool first) {   // n = 0: the second half of the keys
+        const uint32_t a = tm + t * 128 + 64 + 32 * n;
+        const uint64_t b = v0 + ((st * L::kTile + 8192 * (1 - n)) >> 4);
 #pragma unroll
         for (int k = 0; k < 4; ++k) mma_f16_ts<PAIR>(tm + 256 + t * 128, a + 8 * k, b + 128 * k, kIdO, !first || k > 0);
       };
@@ -527,15 +570,18 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         const int st = j % kPreStages, s1 = (j + 1) % kPreStages;
         const bool more = j + 1 < nt;
         ok = wait(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
-        if (ok && more) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
 #pragma unroll 1
         for (int t = 0; t < halves && ok; ++t) {
-          ok = wait(&S.pfull[t][1], j, kDevTimeoutTmemEmpty);
-          if (ok && leader) mma_o(t, st, 1, j == 0);
-          __syncwarp();
-          if (ok) ok = wait(&S.pfull[t][0], j, kDevTimeoutTmemEmpty);
+          ok = wait(&S.pfull[t][0], j, kDevTimeoutTmemEmpty);
           if (ok && leader) {
-            mma_o(t, st, 0, false);
+            mma_o(t, st, 0, j == 0);
+            commit(&S.phalf[t]);
+          }
+          __syncwarp();
+          if (ok && more && t == 0) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
+          if (ok) ok = wait(&S.pfull[t][1], j, kDevTimeoutTmemEmpty);
+          if (ok && leader) {
+            mma_o(t, st, 1, false);
             if (more) {
               mma_s(t, s1);
               commit(&S.sfull[t]);
