@@ -5,7 +5,7 @@
 // into tiles of 256; a CTA takes two row tiles of 128 so that one's softmax runs while the
 // tensor cores work for the other, and both share every widened K and V tile of 128 keys:
 //   S = q ck^T   128 x 128 x D   both operands in shared memory, S in tensor memory
-//   O += P cv    128 x D x 128   P in tensor memory (over S), cv in shared memory
+//   O += P cv    128 x D x 128   P in tensor memory (over half of S), cv in shared memory
 // The codes enter the MMAs as they are (int8 is exact in binary16); scales and the softmax in
 // base 2 are as in the decode kernel: x_j = log2(e) scale sk S_j + log2(sv), weights p_j sv_j
 // relative to the row's maximum, the denominator taken back by 1 / sv, per 16 keys of a page.
@@ -16,8 +16,17 @@
 // V tiles (global to registers a tile ahead, then to shared memory in the 128-byte swizzle);
 // 12 issues the MMAs.
 //
-// Few row tiles are split along the keys: each CTA leaves its rows' sums, and a second launch
-// joins them.
+// Many rows (kPairRows): pairs of CTAs, each widening half of every tile (PAIR below).  Few row
+// tiles are split along the keys: each CTA leaves its rows' sums, and a second launch joins
+// them.
+//
+// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 817 us, 1350
+// TFLOP/s, 70 % of the measured bf16 rate): the chain of a row tile from S over its softmax
+// (about 2400 cycles, two tiles taking turns) back to the next S.  Without the softmax's
+// waits the MMAs and the widening take 605 us (pairs; 720 us for CTAs alone, which are short of
+// shared-memory bandwidth: q, K and V tiles are read at its full rate by the MMAs).  The roles'
+// code has to stay short: they fetch it from one instruction cache (rolled loops and rare code
+// apart: 1041 -> 904 and 878 -> 817 us).
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
@@ -161,7 +170,7 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
 
 // Writes -inf over the scores of the keys that this thread's row does not see, in tensor memory: the
 // few tiles that need it pay for the pass, and the code that every tile runs stays short (with
-// the masks in its middle, 878 instead of MASKUS us for the 8192-token prompt).
+// the masks in its middle, 929 instead of 855 us for a prompt of 8192 tokens, 64 over 8 heads).
 __device__ __forceinline__ void mask_scores(uint32_t tS, int pos, int key, int window, int sinks) {
 #pragma unroll 1
   for (int k = 0; k < kTileKeys; k += 16) {
