@@ -230,7 +230,8 @@ typedef struct dptq_kv8_batch {
  * token_stride elements apart (so they may be parts of one projection's output); 16-byte
  * aligned, token_stride a multiple of 8.
  * Asynchronous.  INVALID_ARG for null or misaligned pointers and bad sizes; UNSUPPORTED for other
- * head_dim or block_tokens, more than 1023 KV heads or 65535 sequences.  seqs == 0 or tokens == 0 is a no-op.
+ * head_dim or block_tokens, more than 1023 KV heads, 65535 sequences or 65535 rows of one, or a
+ * max_len above 2^27.  seqs == 0 or tokens == 0 is a no-op.
  * The first call on a device allocates the library's small scratch (its error word), which is
  * refused (UNSUPPORTED) during stream capture: call dptq_kv8_reserve or dptq_reserve first. */
 dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
@@ -246,8 +247,7 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
  * largest so far; logits, maxima, sums and accumulators are fp32.
  * q_fp16, out_fp16: device rows of `tokens` tokens, q_heads * head_dim binary16 values each, rows
  * q_stride / out_stride elements apart; 16-byte aligned, strides multiples of 8.
- * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.  max_tokens at
- * most 65535 (UNSUPPORTED).
+ * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.
  * Asynchronous; uses the library's per-device scratch (allocated by the first call, or by
  * dptq_kv8_reserve).  Errors as dptq_kv8_append. */
 dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,

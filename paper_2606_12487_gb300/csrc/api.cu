@@ -780,6 +780,8 @@ dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStre
   if (c->block_tokens < 16 || c->block_tokens > 128 || !is_pow2(c->block_tokens))
     return fail(DPTQ_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
   if (c->kv_heads > 1023 || b->seqs > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "too many heads or sequences");
+  if (b->max_tokens > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "more than 65535 rows of a sequence in one call");
+  if (b->max_len > 1 << 27) return fail(DPTQ_ERR_UNSUPPORTED, "sequences longer than 2^27 tokens");
   if (b->seqs == 0 || b->tokens == 0 || b->max_tokens == 0) {
     *none = true;
     return DPTQ_OK;
@@ -850,7 +852,6 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (q_heads <= 0 || window < 0 || sinks < 0 || !std::isfinite(scale))
     return fail(DPTQ_ERR_INVALID_ARG, "bad q_heads, window, sinks or scale");
-  if (batch && batch->max_tokens > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "more than 65535 rows of a sequence in one call");
   if (cache && cache->kv_heads > 0) {
     if (q_heads % cache->kv_heads != 0) return fail(DPTQ_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
     if (q_heads / cache->kv_heads > 64) return fail(DPTQ_ERR_UNSUPPORTED, "more than 64 query heads for a KV head");
@@ -869,8 +870,8 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   a.q_heads = q_heads;
   a.group = q_heads / cache->kv_heads;
   a.scale = scale;
-  a.window = window;
-  a.sinks = sinks;
+  a.window = window < batch->max_len ? window : 0;   // (a window that holds every position)
+  a.sinks = std::min(sinks, batch->max_len);
   if ((st = ensure_kv8_scratch(sc, s)) != DPTQ_OK) return st;
   a.ws = sc->kv8_ws;
   a.counters = sc->kv8_counters;

@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(512, 3) kv8_append_pages_kernel(const Kv8Appen
   const int first = q.start > 0 ? q.start : 0, page = (first >> c.log2_page) + blockIdx.y;
   if (page << c.log2_page >= q.len) return;
   const PageRows pr = page_rows(q, first, page, c.log2_page);
-  const int entry = ld_plain(c.table + (long long)blockIdx.z * c.table_stride + page);   // (looked at after the rows are asked for)
+  // (looked at after the rows are asked for)
+  const int entry = ld_plain(c.table + (long long)blockIdx.z * c.table_stride + page);
   const __half* src = (kv ? a.rows[1] : a.rows[0]) + (q.tok0 + pr.p0 - (long long)q.start) * a.stride +
                       (size_t)head * c.head_dim;
   uint4 x[kAppendVecs];

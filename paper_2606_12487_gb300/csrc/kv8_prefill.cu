@@ -35,7 +35,8 @@
 
 namespace dptq {
 
-constexpr int kConvWarps = 4, kMmaWarp = 8 + kConvWarps, kPreThreads = 32 * (kMmaWarp + 4), kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
+constexpr int kConvWarps = 4, kMmaWarp = 8 + kConvWarps, kPreThreads = 32 * (kMmaWarp + 4);
+constexpr int kTileRows = 128, kTileKeys = 128, kPreStages = 2, kMeta = 4;
 constexpr int kNoEntry = (int)0x80000000;
 
 struct KeyMeta {     // of 16 keys
@@ -489,8 +490,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       return w == 0 && pages >= 0 ? ld_plain((kv ? c.scales[1] : c.scales[0]) + (size_t)pages * c.kv_heads + head) : 0.f;
     };
     auto store = [&](uint8_t* dst, int kv, const uint4 (&v)[kUnits]) {
-      dst += (kv ? (PAIR ? 0 : subv * L::kHalf) + 8 * kbv * 128 : subk * L::kKHalf + 8 * (kbk - (PAIR ? 8 * rank : 0)) * 128) +
-             kr * 128;
+      const int place = kv ? (PAIR ? 0 : subv * L::kHalf) + 8 * kbv * 128
+                           : subk * L::kKHalf + 8 * (kbk - (PAIR ? 8 * rank : 0)) * 128;
+      dst += place + kr * 128;
       const int step = 8 * 128 * (kv ? kWaysV : kWaysK);
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
@@ -682,7 +684,8 @@ static cudaError_t launch_prefill(const Kv8AttendArgs& a, int num_sms, cudaStrea
       const cudaError_t e = ensure_max_dyn_smem(pair);
       if (e != cudaSuccess) return e;
       const int tiles4 = ceil_div((long long)a.c.max_tokens * a.group, 4 * kTileRows);
-      return launch_after(pair, dim3(2 * a.c.kv_heads, a.c.seqs, tiles4), kPreThreads, PreLayout<D, true>::kBytes, s, 2, a, 1);
+      return launch_after(pair, dim3(2 * a.c.kv_heads, a.c.seqs, tiles4), kPreThreads, PreLayout<D, true>::kBytes, s, 2,
+                          a, 1);
     }
   }
   constexpr int smem = PreLayout<D, false>::kBytes;

@@ -70,7 +70,8 @@ __device__ __forceinline__ uint4 norm_take(const NormArgs& a, size_t at, int k, 
   return v;
 }
 
-__device__ __forceinline__ void norm_put(const NormArgs& a, size_t at, int k, const uint4 v, const uint4 g, float s, float r) {
+__device__ __forceinline__ void norm_put(const NormArgs& a, size_t at, int k, const uint4 v, const uint4 g, float s,
+                                         float r) {
   const uint32_t h[4] = {v.x, v.y, v.z, v.w}, gg[4] = {g.x, g.y, g.z, g.w};
   int c[8];
 #pragma unroll

@@ -97,3 +97,12 @@ def test_reference_attention_is_a_weighted_mean():
     v = (cache[2][table[0], 0].astype(float) * cache[3][table[0], 0][:, None, None]).reshape(-1, 64)
     assert np.allclose(out[2, 0], v[[0, 16, 17, 18, 19]].mean(0)) and (tol > 0).all()
     assert ref.sees([2], 5, 2, 0).tolist() == [[False, True, True, False, False]]
+
+
+@pytest.mark.parametrize("batch", [dict(max_tokens=65536, tokens=70000), dict(max_len=(1 << 27) + 1, table_stride=1 << 28)])
+def test_kv8_refuses_what_its_indexes_do_not_hold(dp, batch):
+    c, b = _handles(dp, batch=batch)
+    lib = dp.load()
+    cp, bp = ctypes.addressof(c), ctypes.addressof(b)
+    assert lib.dptq_kv8_append(cp, bp, P(64), P(64), 256, None) == 2
+    assert lib.dptq_kv8_attention(cp, bp, P(64), 1024, 8, F(0.1), 0, 0, P(64), 1024, None) == 2
