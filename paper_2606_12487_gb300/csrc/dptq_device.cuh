@@ -206,6 +206,8 @@ __device__ __forceinline__ bool elect_one() {
 
 // ------------------------------------------------------------------ clusters
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+// (orders nothing: where only the other CTA's progress counts, and not its stores)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // The address in CTA `rank` of the cluster of this CTA's shared address.
 __device__ __forceinline__ uint32_t cluster_map(uint32_t saddr, uint32_t rank) {

@@ -83,10 +83,10 @@ __global__ void __launch_bounds__(512, 3) kv8_append_pages_kernel(const Kv8Appen
   float am = 0.f;
 #pragma unroll
   for (int i = 0; i < kAppendVecs; ++i) {
-    const int v = tid + i * blockDim.x, row = v >> log2v;
-    x[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (row >= pr.lo && row < pr.hi)
-      x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (v & (vecs - 1)));
+    // (always a row that is there: a load in a branch would wait for its own data; rows twice do
+    // not change the maximum)
+    const int v = tid + i * blockDim.x, row = min(max(v >> log2v, pr.lo), pr.hi - 1);
+    x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (v & (vecs - 1)));
   }
   if (entry < 0 || entry >= c.num_blocks) {
     atomicCAS(c.err, 0, kDevBadPage);
@@ -141,11 +141,11 @@ __global__ void __launch_bounds__(256) kv8_append_few_kernel(const Kv8AppendArgs
     float am = 0.f;
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
-      const int row = pr.lo + i * per + (lane >> log2v);
-      x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < pr.hi) x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (lane & (vecs - 1)));
-      am = abs_max8(x[i], am);
+      const int row = min(pr.lo + i * per + (lane >> log2v), pr.hi - 1);   // (a row that is there)
+      x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (lane & (vecs - 1)));
     }
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) am = abs_max8(x[i], am);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
     const float s1 = fmaxf(s0, __fmul_rn(am, 1.f / 127.f)), r = s1 > 0.f ? __frcp_rn(s1) : 0.f;

@@ -216,12 +216,12 @@ kv8_decode_kernel(const Kv8AttendArgs A) {
       int pos[RT][2];   // positions of the two rows whose logits this lane holds
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const int row = g + 8 * r, tok = row / A.group, hh = row - tok * A.group;
+        // (lanes without a row read the first one: a load in a branch would wait for its own data)
+        const int row = g + 8 * r < rows ? g + 8 * r : 0, tok = row / A.group, hh = row - tok * A.group;
         const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          uint2 v = make_uint2(0u, 0u);
-          if (row < rows) v = ld_plain(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
+          const uint2 v = ld_plain(reinterpret_cast<const uint2*>(src + D / 4 * t + 4 * k));
           qf[r][k][0] = v.x;
           qf[r][k][1] = v.y;
         }

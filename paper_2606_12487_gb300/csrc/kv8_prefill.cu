@@ -281,15 +281,23 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     if (t < halves && nt > 0) {
-      {   // this row of q, negated for a negative scale
+      {   // the warp's rows of q, whole rows at a time, negated for a negative scale
+        constexpr int kLanes = D / 8, kSide = 32 / kLanes;   // 16-byte chunks of a row; rows side by side
         const uint32_t flip = A.scale < 0.f ? 0x80008000u : 0u;
-        const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D;
-        uint8_t* dst = sm + L::kQ + t * L::kQTile + r * 128;
+        // (rows past the last one read the tile's first row: a load in a branch would wait for its own
+        // data, and nobody looks at their result)
+        const int from_row = mine ? row : row0, from_tok = from_row / A.group;
+        const long long at = (long long)(q.tok0 + from_tok) * A.q_stride +
+                             (long long)(head * A.group + from_row - from_tok * A.group) * D;
+        const int ch = lane % kLanes;
+        uint8_t* dst = sm + L::kQ + t * L::kQTile + (ch >> 3) * L::kHalf;
 #pragma unroll
-        for (int ch = 0; ch < D / 8; ++ch) {
-          uint4 v = mine ? ld_plain(reinterpret_cast<const uint4*>(src) + ch) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < 32 / kSide; ++i) {
+          const int from = kSide * i + lane / kLanes, rr = (warp & 3) * 32 + from;
+          const long long src = __shfl_sync(0xffffffffu, at, from);
+          uint4 v = ld_plain(reinterpret_cast<const uint4*>(A.q + src) + ch);
           v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
-          *reinterpret_cast<uint4*>(dst + (ch >> 3) * L::kHalf + (((ch & 7) ^ (r & 7)) << 4)) = v;
+          *reinterpret_cast<uint4*>(dst + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) = v;
         }
         fence_proxy_async_smem();
         tell(&S.qfull[t]);
@@ -509,9 +517,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     };
     // Units in order K 0, V 0, K 1, V 1, ..., each loaded while the one before it is widened.
     uint4 cur[kUnits], nxt[kUnits];
-    int pages = checked(entry_of(0)), next = checked(entry_of(1)), entry = entry_of(2);
-    float sk = scale_of(0, pages), sv = scale_of(1, pages);
+    const int entry0 = entry_of(0), entry1 = entry_of(1);
+    int entry = entry_of(2), pages = checked(entry0), next = checked(entry1);
     if (nt > 0) load(0, 0, pages, nxt);
+    float sk = scale_of(0, pages), sv = scale_of(1, pages);
 #pragma unroll 1
     for (int u = 0; u < 2 * nt; ++u) {
       const int j = u >> 1, kv = u & 1, st = j % kPreStages, par = (j / kPreStages + 1) & 1;
@@ -618,7 +627,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
   }
   __syncthreads();
   if constexpr (PAIR) {   // neither CTA leaves, or frees what the other's MMAs read, before both are done
-    cluster_arrive();
+    cluster_arrive_relaxed();
     cluster_wait();
   }
   tc_fence_after();

@@ -120,12 +120,10 @@ __global__ void __launch_bounds__(kNormThreads, norm_ctas(V)) norm_quant_kernel(
   float sq = 0.f, am = 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int k = 8 * (threadIdx.x + i * blockDim.x);
-    x[i] = r[i] = zero;
-    if (k < a.K) {
-      x[i] = *reinterpret_cast<const uint4*>(a.x + at + k);
-      if (a.residual) r[i] = *reinterpret_cast<const uint4*>(a.residual + at + k);
-    }
+    // (threads past the row's end read its last vector: a load in a branch would wait for its data)
+    const int k = min(8 * (int)(threadIdx.x + i * blockDim.x), a.K - 8);
+    x[i] = *reinterpret_cast<const uint4*>(a.x + at + k);
+    r[i] = a.residual ? *reinterpret_cast<const uint4*>(a.residual + at + k) : zero;
   }
   auto weight = [&](int k) { return a.gamma ? ld_plain(reinterpret_cast<const uint4*>(a.gamma + k)) : zero; };
 #pragma unroll
