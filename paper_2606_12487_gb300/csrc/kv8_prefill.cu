@@ -20,8 +20,8 @@
 // tiles are split along the keys: each CTA leaves its rows' sums, and a second launch joins
 // them.
 //
-// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 817 us, 1350
-// TFLOP/s, 70 % of the measured bf16 rate): the chain of a row tile from S over its softmax
+// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 802 us, 1370
+// TFLOP/s, 72 % of the measured bf16 rate): the chain of a row tile from S over its softmax
 // (about 2400 cycles, two tiles taking turns) back to the next S.  Without the softmax's
 // waits the MMAs and the widening take 605 us (pairs; 720 us for CTAs alone, which are short of
 // shared-memory bandwidth: q, K and V tiles are read at its full rate by the MMAs).  The roles'
