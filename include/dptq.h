@@ -242,6 +242,8 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
  *   logit_j = scale * k_scale * (q . k_code_j);  out = sum_j softmax(logit)_j v_scale v_code_j
  * over the keys j that the query at position p sees: j <= p and, with window > 0,
  * j > p - window or j < sinks.  A query that sees none gets zeros.
+ * A page with an infinite scale reads as NaN; scales below 2^-40 count as 2^-40 in V (no binary16 is
+ * lost by it), and NaN in q stays in its row.
  * The integer codes enter the tensor cores exactly (int8 fits in binary16), the scales are
  * applied in fp32; softmax weights times V scale are rounded to binary16 relative to their
  * largest so far; logits, maxima, sums and accumulators are fp32.
