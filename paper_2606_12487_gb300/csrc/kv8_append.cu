@@ -20,7 +20,7 @@
 namespace dptq {
 
 constexpr int kAppendVecs = 4;    // 16-byte vectors of a thread
-constexpr int kAppendFew = 8;
+constexpr int kAppendFew = 8;     // (8 tokens of each of 128 sequences, 32 heads: 7.3 us a call; a CTA a page: 30.8)
 
 // The new rows of a page of a sequence.
 struct PageRows {

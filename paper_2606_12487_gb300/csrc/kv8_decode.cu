@@ -38,9 +38,10 @@ namespace dptq {
 
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 constexpr int kDecKeys = 32;        // keys of a step
-constexpr int kDecMinSteps = 4;     // fewest steps that a CTA is started for: one a warp
-constexpr int kDecJoin = 12;        // most partial results joined at once
-constexpr int kDecJoinMost = 32;    // of a group, and groups: sqrt of a grid of 1024 CTAs at most
+// Fewest steps that a CTA is started for: one a warp (one sequence of 512 tokens, 8 heads: 9.4 us; 8 steps:
+// 10.6 us).  Most partial results joined at once (57 of one sequence of 131072 tokens in two levels: 54.9 us;
+// in one: 59.3 us), and of a group, or groups: sqrt of a grid of 1024 CTAs at most.
+constexpr int kDecMinSteps = 4, kDecJoin = 12, kDecJoinMost = 32;
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {

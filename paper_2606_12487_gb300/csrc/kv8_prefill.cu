@@ -672,7 +672,11 @@ __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, in
   for (int e = 0; e < E; e += 2) *reinterpret_cast<__half2*>(dst + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
 }
 
-constexpr int kPairRows = 512;   // rows of a sequence and KV head from which pairs of CTAs take them
+// Rows of a sequence and KV head from which pairs of CTAs take them.  Pairs / CTAs alone, us, 64 over 8
+// heads: 16 sequences x 64 new tokens behind 4000: 118 / 133; 16 x 256: 363 / 399; 1 x 2048 behind 8000:
+// 464 / 526; 2 x 4096: 357 / 383; 4 x 1024: 83 / 80.  Pairs lose where sequences of one or two pair tiles
+// round up into another wave: 16 x about 100 behind 4000: 228 / 200.
+constexpr int kPairRows = 512;
 
 template <int D>
 static cudaError_t launch_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s) {
