@@ -20,8 +20,8 @@
 // tiles are split along the keys: each CTA leaves its rows' sums, and a second launch joins
 // them.
 //
-// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 802 us, 1370
-// TFLOP/s, 72 % of the measured bf16 rate): the chain of a row tile from S over its softmax
+// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 808 us, 1361
+// TFLOP/s, 71 % of the measured bf16 rate): the chain of a row tile from S over its softmax
 // (about 2400 cycles, two tiles taking turns) back to the next S.  Without the softmax's
 // waits the MMAs and the widening take 605 us (pairs; 720 us for CTAs alone, which are short of
 // shared-memory bandwidth: q, K and V tiles are read at its full rate by the MMAs).  The roles'
@@ -46,6 +46,7 @@ struct KeyMeta {     // of 16 keys
 struct PreShared {
   KeyMeta meta[kMeta][kTileKeys / 16];
   uint64_t kfull[kPreStages], kempty[kPreStages], vfull[kPreStages], vempty[kPreStages];
+  uint64_t mfull[kMeta];   // meta is there (filled and read within a CTA)
   uint64_t qfull[2], sfull[2], pfull[2][2], ofull[2], drain;   // pfull: the two halves of a tile's keys
   uint64_t phalf[2];   // the first half's product is complete
   uint32_t tmem;
@@ -132,9 +133,9 @@ __device__ __forceinline__ void reg_less() {
 // mbar_wait_warp in few instructions (the bound counts polls, of 64 cycles and more each): the
 // roles' loops together have to stay in the instruction cache.  With everything unrolled the
 // MMA warp spent more time on fetching its code than on issuing it.
-__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
-                                               int code, long long limit) {
-  for (long long polls = limit >> 6; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); --polls) {
+template <class Arrived>
+__device__ __forceinline__ bool wait_near(Arrived arrived, volatile int* abort_flag, int* err, int code, long long limit) {
+  for (long long polls = limit >> 6; !__all_sync(0xffffffffu, arrived()); --polls) {
     __nanosleep(20);
     if (__any_sync(0xffffffffu, *abort_flag != 0 || polls <= 0)) {
       *abort_flag = 1;
@@ -143,6 +144,25 @@ __device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, v
     }
   }
   return true;
+}
+__device__ __forceinline__ bool mbar_wait_near(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                               int code, long long limit) {
+  return wait_near([&] { return mbar_try_wait(bar, parity); }, abort_flag, err, code, limit);
+}
+// What the arrivals released at cluster scope is seen (mbar_arrive_remote_release).
+__device__ __forceinline__ bool mbar_wait_near_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err,
+                                                       int code, long long limit) {
+  return wait_near([&] { return mbar_try_wait_cluster(bar, parity); }, abort_flag, err, code, limit);
+}
+// Two barriers, whose answers come back together.
+__device__ __forceinline__ bool mbar_wait2_near(uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1,
+                                                volatile int* abort_flag, int* err, int code, long long limit) {
+  return wait_near(
+      [&] {
+        const bool r0 = mbar_try_wait(b0, p0), r1 = mbar_try_wait(b1, p1);
+        return r0 && r1;
+      },
+      abort_flag, err, code, limit);
 }
 
 // The 128-key tiles that a CTA's rows see: `sink` tiles from key 0, then tiles from key `from`.
@@ -201,8 +221,10 @@ struct PreLayout {
 // PAIR: two CTAs of a cluster work on 512 rows, 256 each; the tensor cores of both take K and V
 // tiles of which each CTA widens and holds one half (of K's keys, of V's dims).  That halves the
 // widening, its stores and what the MMAs read of K and V from shared memory, which is what a
-// CTA alone is short of.  The first CTA issues the MMAs; the second one's widening and softmax
-// warps arrive on its barriers (mbar_arrive_remote says what that rests on).
+// CTA alone is short of.  The first CTA issues the MMAs.  What the second one stores for them reaches
+// its barriers in three ways: q, once, released at cluster scope; K and V on the second CTA's own
+// barriers, from which its MMA warp, which has no loads under way, passes them on released at cluster
+// scope; P, stores to tensor memory, as mbar_arrive_remote says.
 template <int D, bool SPLIT, bool PAIR>
 __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8AttendArgs A, int nsplit) {
   static_assert(!PAIR || (D == 128 && !SPLIT), "a pair's halves of V are 64 dims; few rows take no pairs");
@@ -231,11 +253,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 
   if (tid == 0) {
     for (int i = 0; i < kPreStages; ++i) {
-      mbar_init(&S.kfull[i], kCtas * kConvWarps);
-      mbar_init(&S.vfull[i], kCtas * kConvWarps);
+      mbar_init(&S.kfull[i], kConvWarps + (PAIR && rank == 0 ? 1 : 0));   // (and the second CTA's MMA warp)
+      mbar_init(&S.vfull[i], kConvWarps + (PAIR && rank == 0 ? 1 : 0));
       mbar_init(&S.kempty[i], 1);
       mbar_init(&S.vempty[i], 1);
     }
+    for (int i = 0; i < kMeta; ++i) mbar_init(&S.mfull[i], 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&S.qfull[t], kCtas * kTileRows / 32);
       mbar_init(&S.pfull[t][0], kCtas * kTileRows / 32);
@@ -256,14 +279,17 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     cluster_wait();
   }
   tc_fence_after();
-  // Arrives on a barrier of the CTA that issues the MMAs, for this warp.
-  auto tell = [&](uint64_t* bar) {
+  // Arrives for this warp on a barrier of the CTA that issues the MMAs; stored: for its stores to
+  // shared memory.
+  auto tell_first = [&](uint64_t* bar, bool stored) {
     __syncwarp();
     if (lane == 0) {
-      if (PAIR && rank != 0)
-        mbar_arrive_remote(cluster_map(smem_u32(bar), 0));
-      else
+      if (!PAIR || rank == 0)
         mbar_arrive(bar);
+      else if (stored)
+        mbar_arrive_remote_release(cluster_map(smem_u32(bar), 0));
+      else
+        mbar_arrive_remote(cluster_map(smem_u32(bar), 0));
     }
   };
   const uint32_t tm = S.tmem;   // S of the row tiles at columns 0 and 128, O at 256 and 384
@@ -300,14 +326,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           *reinterpret_cast<uint4*>(dst + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) = v;
         }
         fence_proxy_async_smem();
-        tell(&S.qfull[t]);
+        tell_first(&S.qfull[t], true);
       }
       // positions of this row tile's rows
       const int r_lo = (t * kCtas + rank) * kTileRows;
       const int r_hi = r_lo + kTileRows - 1 < nrows - 1 ? r_lo + kTileRows - 1 : nrows - 1;
       const int p_lo = q.start + (row0 + r_lo) / A.group, p_hi = q.start + (row0 + r_hi) / A.group;
       for (int j = 0; j < nt && ok; ++j) {
-        ok = mbar_wait_near(&S.sfull[t], j & 1, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
+        ok = mbar_wait2_near(&S.mfull[j % kMeta], (j / kMeta) & 1, &S.sfull[t], j & 1, abort_flag, c.err,
+                             kDevTimeoutTmemFull, A.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         const int key = all.key(j0 + j);
@@ -385,7 +412,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
             if (n == 0) tmem_ld32(tS, xa);
             tmem_st_wait();
             tc_fence_before();
-            tell(&S.pfull[t][n]);
+            tell_first(&S.pfull[t][n], false);
           }
           if (n == 2) break;
           const float mn = fmaxf(m, top), f = mn == m ? 1.f : exp2_fast(m - mn);   // (m = -inf: no key yet)
@@ -540,7 +567,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         sv = scale_of(1, next);
       }
       store(sm + (kv ? L::kV : L::kK) + st * L::kTile, kv, cur);
-      tell(kv ? &S.vfull[st] : &S.kfull[st]);
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(kv ? &S.vfull[st] : &S.kfull[st]);
+        // (here, and not where the scales are stored: 840 instead of 808 us for the long prompt)
+        if (w == 0 && kv == 0) mbar_arrive(&S.mfull[j % kMeta]);
+      }
       if (kv) {
         pages = next;
         next = checked(entry);
@@ -556,6 +588,12 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       const bool leader = elect_one();
       auto wait = [&](uint64_t* bar, int par, int code) {
         const bool ok = mbar_wait_near(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
+        tc_fence_after();
+        return ok;
+      };
+      auto wait_stored = [&](uint64_t* bar, int par, int code) {   // (for both CTAs' shared memory)
+        const bool ok = PAIR ? mbar_wait_near_cluster(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles)
+                             : mbar_wait_near(bar, (uint32_t)par & 1u, abort_flag, c.err, code, A.wait_cycles);
         tc_fence_after();
         return ok;
       };
@@ -575,9 +613,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 #pragma unroll
         for (int k = 0; k < 4; ++k) mma_f16_ts<PAIR>(tm + 256 + t * 128, a + 8 * k, b + 128 * k, kIdO, !first || k > 0);
       };
-      bool ok = wait(&S.kfull[0], 0, kDevTimeoutConv);
+      bool ok = wait_stored(&S.kfull[0], 0, kDevTimeoutConv);
       for (int t = 0; t < halves && ok; ++t) {
-        ok = wait(&S.qfull[t], 0, kDevTimeoutFull);
+        ok = wait_stored(&S.qfull[t], 0, kDevTimeoutFull);
         if (ok && leader) {
           mma_s(t, 0);
           commit(&S.sfull[t]);
@@ -589,7 +627,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       for (int j = 0; j < nt && ok; ++j) {
         const int st = j % kPreStages, s1 = (j + 1) % kPreStages;
         const bool more = j + 1 < nt;
-        ok = wait(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
+        ok = wait_stored(&S.vfull[st], j / kPreStages, kDevTimeoutConv);
 #pragma unroll 1
         for (int t = 0; t < halves && ok; ++t) {
           ok = wait(&S.pfull[t][0], j, kDevTimeoutTmemEmpty);
@@ -598,7 +636,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
             commit(&S.phalf[t]);
           }
           __syncwarp();
-          if (ok && more && t == 0) ok = wait(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
+          if (ok && more && t == 0) ok = wait_stored(&S.kfull[s1], (j + 1) / kPreStages, kDevTimeoutConv);
           if (ok) ok = wait(&S.pfull[t][1], j, kDevTimeoutTmemEmpty);
           if (ok && leader) {
             mma_o(t, st, 1, false);
@@ -622,6 +660,16 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         __syncwarp();
         int no_abort = 0;
         mbar_wait_warp(&S.drain, 0, &no_abort, c.err, kDevTimeoutDrain, A.wait_cycles);
+      }
+    } else if (PAIR && warp == kMmaWarp) {
+      // ------------------------------------------------------------------ the second CTA's units, passed on
+#pragma unroll 1
+      for (int u = 0; u < 2 * nt; ++u) {   // K 0, V 0, K 1, V 1, ..., as they are widened
+        const int j = u >> 1, st = j % kPreStages;
+        uint64_t* bar = u & 1 ? &S.vfull[st] : &S.kfull[st];
+        if (!mbar_wait_near(bar, (j / kPreStages) & 1, abort_flag, c.err, kDevTimeoutConv, A.wait_cycles)) break;
+        if (lane == 0) mbar_arrive_remote_release(cluster_map(smem_u32(bar), 0));
+        __syncwarp();
       }
     }
   }
