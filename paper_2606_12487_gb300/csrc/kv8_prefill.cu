@@ -655,12 +655,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
           __syncwarp();
         }
       }
-      if (!ok) {   // a wait gave up: the MMAs under way end before tensor memory is freed
-        if (leader) commit(&S.drain);
-        __syncwarp();
-        int no_abort = 0;
-        mbar_wait_warp(&S.drain, 0, &no_abort, c.err, kDevTimeoutDrain, A.wait_cycles);
-      }
+      if (leader) commit(&S.drain);
+      __syncwarp();
     } else if (PAIR && warp == kMmaWarp) {
       // ------------------------------------------------------------------ the second CTA's units, passed on
 #pragma unroll 1
@@ -671,6 +667,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
         if (lane == 0) mbar_arrive_remote_release(cluster_map(smem_u32(bar), 0));
         __syncwarp();
       }
+    }
+    if (warp == kMmaWarp && nt > 0) {
+      // The MMAs and their arrivals (in both CTAs) end before tensor memory is freed and the CTA
+      // leaves, whichever warp's wait gave up: also the last ones', which only the softmax waits for.
+      // (the full bound, whatever the caller's is)
+      int no_abort = 0;
+      mbar_wait_warp(&S.drain, 0, &no_abort, c.err, kDevTimeoutDrain);
     }
   }
   __syncthreads();
