@@ -412,6 +412,15 @@ int take_rows_shortfall() {
   return left.exchange(0);
 }
 
+// DPTQ_TEST_KV8_SHORTFALL=abc: the digits, one for each call of dptq_kv8_attention.
+int take_kv8_shortfall() {
+  static const char* const v = std::getenv("DPTQ_TEST_KV8_SHORTFALL");
+  if (v == nullptr) return 0;
+  static std::atomic<size_t> calls{0};
+  const size_t i = calls++;
+  return i < std::strlen(v) ? v[i] - '0' : 0;
+}
+
 cudaError_t ensure_max_dyn_smem_impl(const void* fn) {
   // One entry per (kernel, device) whose ceiling is already raised.
   static std::mutex mu;
@@ -876,6 +885,7 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   a.ws = sc->kv8_ws;
   a.counters = sc->kv8_counters;
   a.wait_cycles = wait_cycles_setting();
+  a.shortfall = take_kv8_shortfall();
   const bool decode = (long long)a.c.max_tokens * a.group <= kDecodeRows;
   DPTQ_CUDA(decode ? launch_kv8_decode(a, sc->num_sms, s) : launch_kv8_prefill(a, sc->num_sms, s), "kv8_attention launch");
   return DPTQ_OK;

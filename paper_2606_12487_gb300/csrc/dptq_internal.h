@@ -145,6 +145,8 @@ struct Kv8AttendArgs {
   float* ws;               // partial results of shared (sequence, head)s
   uint32_t* counters;      // their arrivals (zero between launches)
   long long wait_cycles;   // bound of a pipeline wait (SM cycles) before the kernel gives up
+  int shortfall;           // test hook: a barrier of a prompt's kernel that waits for one arrival more
+                           // than there is (1: widened K, 2: the weights, 3: the output; 0: none)
 };
 // Most rows of a (sequence, KV head) in the decode kernel: 16 rows of 64 sequences of 8000 tokens, 8 KV heads,
 // take 210 us there and 458 us in the prompt kernel, whose row tiles are 128 rows.
@@ -245,6 +247,7 @@ long long wait_cycles_setting();
 // for n more published token rows than any CTA publishes, so that its bounded wait runs
 // out (returns n once, then 0).
 int take_rows_shortfall();
+int take_kv8_shortfall();
 bool decode_whole_tiles();   // DPTQ_DECODE_WHOLE_TILES=0: decode grids never shrink to one CTA per tile
 bool a8_tile128();   // DPTQ_A8_TILE128=1: A8 prefill on 128-token tiles (weights widened into shared memory)
 // Activation rows are rotated by the tensor-core kernel unless DPTQ_ROWS_KERNEL=0 (the

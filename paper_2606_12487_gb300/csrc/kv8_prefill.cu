@@ -130,14 +130,17 @@ __device__ __forceinline__ void reg_less() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-// mbar_wait_warp in few instructions (the bound counts polls, of 64 cycles and more each): the
+// mbar_wait_warp in few instructions (its clock starts at the first poll that finds nothing): the
 // roles' loops together have to stay in the instruction cache.  With everything unrolled the
-// MMA warp spent more time on fetching its code than on issuing it.
+// MMA warp spent more time on fetching its code than on issuing it.  The bound is in cycles: a poll
+// may be suspended for any time, so that a number of polls bounds nothing.
 template <class Arrived>
 __device__ __forceinline__ bool wait_near(Arrived arrived, volatile int* abort_flag, int* err, int code, long long limit) {
-  for (long long polls = limit >> 6; !__all_sync(0xffffffffu, arrived()); --polls) {
+  for (long long t0 = 0; !__all_sync(0xffffffffu, arrived());) {
+    const long long now = clock64();
+    if (t0 == 0) t0 = now;
     __nanosleep(20);
-    if (__any_sync(0xffffffffu, *abort_flag != 0 || polls <= 0)) {
+    if (__any_sync(0xffffffffu, *abort_flag != 0 || now - t0 > limit)) {
       *abort_flag = 1;
       atomicCAS(err, 0, code);
       return false;
@@ -253,7 +256,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
 
   if (tid == 0) {
     for (int i = 0; i < kPreStages; ++i) {
-      mbar_init(&S.kfull[i], kConvWarps + (PAIR && rank == 0 ? 1 : 0));   // (and the second CTA's MMA warp)
+      mbar_init(&S.kfull[i], (A.shortfall == 1) + kConvWarps + (PAIR && rank == 0 ? 1 : 0));   // (and the second CTA's MMA warp)
       mbar_init(&S.vfull[i], kConvWarps + (PAIR && rank == 0 ? 1 : 0));
       mbar_init(&S.kempty[i], 1);
       mbar_init(&S.vempty[i], 1);
@@ -262,10 +265,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     for (int t = 0; t < 2; ++t) {
       mbar_init(&S.qfull[t], kCtas * kTileRows / 32);
       mbar_init(&S.pfull[t][0], kCtas * kTileRows / 32);
-      mbar_init(&S.pfull[t][1], kCtas * kTileRows / 32);
+      mbar_init(&S.pfull[t][1], (A.shortfall == 2) + kCtas * kTileRows / 32);
       mbar_init(&S.sfull[t], 1);
       mbar_init(&S.phalf[t], 1);
-      mbar_init(&S.ofull[t], 1);
+      mbar_init(&S.ofull[t], (A.shortfall == 3) + 1);
     }
     mbar_init(&S.drain, 1);
     S.abort = 0;
