@@ -192,6 +192,14 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
 }
 
+// The addend b of a page whose V scale is infinite.  It is finite, so that a masked S = -inf still gives
+// x = -inf (+inf would give NaN to rows that do not see the page); a row that sees such a key ends
+// with it as its maximum, and no other row gets near it: those rows' results are NaN.
+constexpr float kNoNumber = 3.402823466e38f;
+__device__ __forceinline__ float one_over_sum(float m, float l) {
+  return m >= kNoNumber ? __int_as_float(0x7FFFFFFF) : l == 0.f ? 0.f : __frcp_rn(l);
+}
+
 // Writes -inf over the scores of the keys that this thread's row does not see, in tensor memory: the
 // few tiles that need it pay for the pass, and the code that every tile runs stays short (with
 // the masks in its middle, 929 instead of 855 us for a prompt of 8192 tokens, 64 over 8 heads).
@@ -447,7 +455,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     }
     // ---- output
     if (ok && t < halves) {
-      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+      const float inv = one_over_sum(m, l);
       __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D;
       float* part = nullptr;
       if constexpr (SPLIT) {
@@ -562,9 +570,10 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       if (kv == 0) {
         if (w == 0 && lane < kTileKeys / 16) {
           const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-          // a > 0, so that a masked S = -inf gives x = -inf
-          S.meta[j % kMeta][lane] = {fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f),
-                                     pages >= 0 ? __log2f(s) : -INFINITY, __frcp_rn(s), 0.f};
+          const bool finite = s < INFINITY;
+          // a > 0 and b < inf, so that a masked S = -inf gives x = -inf
+          S.meta[j % kMeta][lane] = {finite ? fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f) : 1e-37f,
+                                     pages < 0 ? -INFINITY : finite ? __log2f(s) : kNoNumber, __frcp_rn(s), 0.f};
         }
         sk = scale_of(0, next);
         sv = scale_of(1, next);
@@ -719,7 +728,7 @@ __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, in
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldcg(p + (size_t)r * D + E * lane + e), o[e]);
   }
-  const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+  const float inv = one_over_sum(M, l);
   const int tok = row / A.group, hh = row - tok * A.group;
   __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D + E * lane;
 #pragma unroll
