@@ -186,7 +186,7 @@ dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16
                                    void* stream);
 
 /* A paged KV cache of int8 codes with one fp32 scale for each page of tokens and KV head:
- * value = scale * code.  Codes [num_blocks][kv_heads][block_tokens][head_dim], 16-byte aligned;
+ * value = scale * code, scale >= 0.  Codes [num_blocks][kv_heads][block_tokens][head_dim], 16-byte aligned;
  * scales [num_blocks][kv_heads].  All device memory of the caller; the struct itself is host
  * memory, read during the call only.  head_dim 64 or 128; block_tokens 16, 32, 64 or 128. */
 typedef struct dptq_kv8_cache {
@@ -242,7 +242,8 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
  *   logit_j = scale * k_scale * (q . k_code_j);  out = sum_j softmax(logit)_j v_scale v_code_j
  * over the keys j that the query at position p sees: j <= p and, with window > 0,
  * j > p - window or j < sinks.  A query that sees none gets zeros.
- * A page with an infinite scale reads as NaN; scales below 2^-40 count as 2^-40 in V (no binary16 is
+ * A query that sees a key of a page whose K or V scale is infinite or NaN gets NaN, whatever the page's
+ * codes are; no other query is touched by it.  Scales below 2^-40 count as 2^-40 in V (no binary16 is
  * lost by it), and NaN in q stays in its row.
  * The integer codes enter the tensor cores exactly (int8 fits in binary16), the scales are
  * applied in fp32; softmax weights times V scale are rounded to binary16 relative to their

@@ -330,7 +330,9 @@ kv8_decode_kernel(const Kv8AttendArgs A) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // per 16 keys one factor and one addend
           const float v = fmaxf(h ? scl.w : scl.z, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-          const float fa = (h ? scl.y : scl.x) * (A.scale * 1.4426950408889634f), fb = __log2f(v);
+          const bool finite = isfinite(h ? scl.y : scl.x) && isfinite(h ? scl.w : scl.z);
+          // (what is not seen is masked below: such a page stays with the rows that see it)
+          const float fa = (h ? scl.y : scl.x) * (A.scale * 1.4426950408889634f), fb = finite ? __log2f(v) : NAN;
           inv[h] = __frcp_rn(v);
 #pragma unroll
           for (int r = 0; r < RT; ++r)

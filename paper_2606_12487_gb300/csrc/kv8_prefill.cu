@@ -192,7 +192,7 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
 }
 
-// The addend b of a page whose V scale is infinite.  It is finite, so that a masked S = -inf still gives
+// The addend b of a page with a scale that is infinite or NaN.  It is finite, so that a masked S = -inf still gives
 // x = -inf (+inf would give NaN to rows that do not see the page); a row that sees such a key ends
 // with it as its maximum, and no other row gets near it: those rows' results are NaN.
 constexpr float kNoNumber = 3.402823466e38f;
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
       if (kv == 0) {
         if (w == 0 && lane < kTileKeys / 16) {
           const float s = fmaxf(sv, 0x1p-40f);   // (below, 127 sv is no binary16 any more)
-          const bool finite = s < INFINITY;
+          const bool finite = isfinite(sk) && isfinite(sv);
           // a > 0 and b < inf, so that a masked S = -inf gives x = -inf
           S.meta[j % kMeta][lane] = {finite ? fmaxf(sk * (fabsf(A.scale) * 1.4426950408889634f), 1e-37f) : 1e-37f,
                                      pages < 0 ? -INFINITY : finite ? __log2f(s) : kNoNumber, __frcp_rn(s), 0.f};

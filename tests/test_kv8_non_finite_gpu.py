@@ -1,5 +1,5 @@
-"""Infinite values that reach the cache: what a row does not see does not touch it, in any form of the
-kernels, and a row that sees a page with an infinite scale is NaN."""
+"""Infinite values that reach the cache, and scales that are no numbers: what a row does not see does not touch it, in any form of the
+kernels, and a row that sees a page with such a scale is NaN."""
 import math
 
 import numpy as np
@@ -72,3 +72,16 @@ def test_an_infinite_value_in_a_prompt_leaves_earlier_tokens_alone(dp, ns, lens,
     page = int(lens[0] - ns[0] + 70) // P
     assert np.isinf(caches[1][3][table[0, page]]).all()
     _check(dp, caches[0], caches[1], q, cu, lens, table, _rows_that_see(lens, ns, page, 0, 0), 0, 0)
+
+
+@pytest.mark.parametrize("ns,lens,H,g,D", FORMS)
+@pytest.mark.parametrize("kv,value", [(1, np.nan), (1, np.inf), (3, np.nan)])
+def test_scales_that_are_no_numbers(dp, ns, lens, H, g, D, kv, value):  # noqa: F811
+    """A caller's own cache: a NaN, or an infinite K scale, whatever the page's codes are."""
+    rng = np.random.default_rng(D + ns[0])
+    cu, lens, table, blocks = ref.random_batch(rng, ns, lens, P)
+    cache = ref.random_cache(rng, blocks, H, P, D)
+    page = int((lens[0] - ns[0] // 2 - 1) // P)
+    dirty = [a.copy() for a in cache]
+    dirty[kv][table[0, page]] = value
+    _check(dp, cache, dirty, _rows(rng, sum(ns), H * g, D), cu, lens, table, _rows_that_see(lens, ns, page, 0, 0), 0, 0)
