@@ -172,8 +172,9 @@ dptq_status dptq_sensitivity_policy(const float* x, const float* dx, int L, int 
  * in fp32 with the IEEE quotient; fl(1 / qmax) is the reciprocal of 7 or 127 rounded to fp32
  * (the quantizers above divide by qmax; a step one unit in the last place away serves as well).
  * The norm's factor is one positive number a token, so it goes into the scale alone and the
- * codes depend on h and gamma only, bit for bit.  A token of zeros has scale 0 and codes 0; a
- * NaN counts for nothing in the maximum and takes the code 0.
+ * codes depend on h and gamma only, bit for bit.  A token of zeros has scale 0 and codes 0, with
+ * eps = 0 too; a NaN counts for nothing in the maximum and takes the code 0, and its token's scale
+ * is NaN.
  * x_fp16, residual_fp16, residual_out: device [M][K] binary16.  residual_fp16 NULL: h = x, and
  *   residual_out must be NULL too; otherwise residual_out receives h and may be x_fp16 or
  *   residual_fp16 itself.  gamma_fp16: device [K], or NULL for 1.

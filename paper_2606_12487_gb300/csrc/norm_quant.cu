@@ -102,7 +102,10 @@ __device__ __forceinline__ void norm_put(const NormArgs& a, size_t at, int k, co
 __device__ __forceinline__ void norm_scale(const NormArgs& a, int row, float sq, float am, float& s, float& r) {
   s = __fmul_rn(am, a.bits == 4 ? 1.f / 7.f : 1.f / 127.f);
   r = s > 0.f ? __frcp_rn(s) : 0.f;
-  if (threadIdx.x == 0) a.scales[row] = s * __frcp_rn(__fsqrt_rn(__fdiv_rn(sq, (float)a.K) + a.eps));
+  // (no square, however small h is, rounds to zero: a sum of zero is a token of zeros, whose factor is 1 / 0
+  // without eps)
+  if (threadIdx.x == 0)
+    a.scales[row] = sq == 0.f ? 0.f : s * __frcp_rn(__fsqrt_rn(__fdiv_rn(sq, (float)a.K) + a.eps));
 }
 
 // A token of at most 8 V blockDim values, in registers.

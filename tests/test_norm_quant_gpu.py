@@ -141,3 +141,25 @@ def test_norm_quant_refusals(dp):
         call(x.float(), None, None, EPS, 8, None, c, s)
     empty = torch.zeros((0, 64), dtype=torch.float16, device="cuda")
     call(empty, None, None, EPS, 8, None, c[:0], s[:0])
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("K", [64, 4096, 20480])
+@pytest.mark.parametrize("eps", [EPS, 0.0])
+def test_a_token_of_zeros_has_scale_zero(dp, bits, K, eps):
+    """With eps = 0 too, where the norm's own factor is 1 / 0; also where only the sum is zero, or only the
+    weighted values are."""
+    rng = np.random.default_rng(K)
+    x = rng.standard_normal((4, K)).astype(np.float16)
+    x[0] = 0
+    r = np.zeros_like(x)
+    r[1] = -x[1]
+    for rr, gg, zero in ((r, None, [0, 1]), (None, None, [0]), (r, np.zeros(K, np.float16), [0, 1, 2, 3])):
+        _, c, s = _call(dp, x, rr, gg, bits, eps)
+        _, c_ref, s_ref = ref.norm_quant(x, rr, gg, eps, bits)
+        assert np.array_equal(c, c_ref) and not c[zero].any() and not s[zero].any()
+        rest = [i for i in range(4) if i not in zero]
+        np.testing.assert_allclose(s[rest], s_ref[rest], rtol=((K / 32 + 32) / 2 + 8) * 2.0 ** -24, atol=0)
+    x[0, 3] = np.nan                             # no number, and nothing else in the token
+    _, c, s = _call(dp, x, None, None, bits, eps)
+    assert not c[0].any() and np.isnan(s[0])
