@@ -370,7 +370,8 @@ dptq_status dptq_get_shape(dptq_handle h, int* N, int* K, int* had_block);
  * per-device scratch of the allocating calls and the fixed array of dptq_qlinear_static;
  * after a timeout it also zeroes the split-tile sums and counters the aborted kernel may
  * have left, so that later calls start clean.  INVALID_ARG: a KV8 call's device arrays held
- * lengths or page numbers out of range. */
+ * lengths or page numbers out of range.  Where both happened, the time-out is the answer and the
+ * arrays are that of the next call. */
 dptq_status dptq_last_device_error(dptq_handle h);
 
 /* Test hook: the activation-plane and scale buffers of the current device's scratch,

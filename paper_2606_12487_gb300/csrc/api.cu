@@ -174,7 +174,7 @@ struct Scratch {
   size_t counter_words = 0;
   uint32_t* gsync = nullptr;
   uint32_t* pmax = nullptr;
-  int* err = nullptr;
+  int* err = nullptr;                 // [2] device error words: waits that gave up; KV8 arrays out of range
   int num_sms = 0;
   float* kv8_ws = nullptr;            // partial attention results and their arrival counters,
   uint32_t* kv8_counters = nullptr;   // from the first attention call or dptq_kv8_reserve on
@@ -234,10 +234,10 @@ dptq_status ensure_scratch(int dev, size_t act_bytes, size_t sa_count, cudaStrea
     int* err = nullptr;
     cudaError_t e = dev_malloc(reinterpret_cast<void**>(&ws), ws_bytes);
     if (e == cudaSuccess) e = dev_malloc(reinterpret_cast<void**>(&counters), sizeof(uint32_t) * counter_words(sms));
-    if (e == cudaSuccess) e = dev_malloc(reinterpret_cast<void**>(&err), sizeof(int));
+    if (e == cudaSuccess) e = dev_malloc(reinterpret_cast<void**>(&err), 2 * sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(ws, 0, ws_bytes);
     if (e == cudaSuccess) e = cudaMemset(counters, 0, sizeof(uint32_t) * counter_words(sms));
-    if (e == cudaSuccess) e = cudaMemset(err, 0, sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(err, 0, 2 * sizeof(int));
     if (e != cudaSuccess) {   // nothing has used these yet: release them and stay uninitialized
       if (ws) cudaFree(ws);
       if (counters) cudaFree(counters);
@@ -823,6 +823,7 @@ dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStre
   a->head_dim = c->head_dim;
   a->log2_page = c->block_tokens == 16 ? 4 : c->block_tokens == 32 ? 5 : c->block_tokens == 64 ? 6 : 7;
   a->err = (*sc)->err;
+  a->bad = (*sc)->err + 1;
   return DPTQ_OK;
 }
 
@@ -1025,13 +1026,16 @@ dptq_status dptq_last_device_error(dptq_handle h) {
   dptq_status st = current_device(&dev);
   if (st != DPTQ_OK) return st;
   DPTQ_CUDA(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
-  int word = 0;
+  int word = 0, bad = 0;
   {
     std::lock_guard<std::mutex> lk(g_mu);
     auto it = g_scratch.find(dev);
     if (it != g_scratch.end() && it->second.err != nullptr) {
       Scratch& sc = it->second;
-      DPTQ_CUDA(cudaMemcpy(&word, sc.err, sizeof(int), cudaMemcpyDeviceToHost), "cudaMemcpy(err)");
+      int words[2];
+      DPTQ_CUDA(cudaMemcpy(words, sc.err, sizeof(words), cudaMemcpyDeviceToHost), "cudaMemcpy(err)");
+      word = words[0];
+      bad = words[1];
       if (word != 0) {
         // A wait gave up: clear the word, the split-tile sums and every counter (split-tile
         // arrivals, the fused launch's two grid counters and its row-maximum slots) the
@@ -1047,14 +1051,18 @@ dptq_status dptq_last_device_error(dptq_handle h) {
   const cudaError_t e = static_scratch_check_reset(dev, &sword);
   if (e != cudaSuccess) return cuda_fail(e, "static scratch error word");
   if (word == 0) word = sword;
-  if (word == 0) return DPTQ_OK;
-  if (word == kDevBadBatch || word == kDevBadPage)
-    return fail(DPTQ_ERR_INVALID_ARG, word == kDevBadPage
-                                          ? "a KV8 call met a page number outside the cache"
-                                          : "a KV8 call's sequence exceeded its declared tokens or length");
-  char buf[64];
-  snprintf(buf, sizeof(buf), "device wait timed out (code 0x%x)", word);
-  return fail(DPTQ_ERR_TIMEOUT, buf);
+  if (word != 0) {   // (a bad array waits for the next question)
+    char buf[64];
+    snprintf(buf, sizeof(buf), "device wait timed out (code 0x%x)", word);
+    return fail(DPTQ_ERR_TIMEOUT, buf);
+  }
+  if (bad == 0) return DPTQ_OK;
+  {
+    std::lock_guard<std::mutex> lk(g_mu);
+    DPTQ_CUDA(cudaMemset(g_scratch[dev].err + 1, 0, sizeof(int)), "cudaMemset(err)");
+  }
+  return fail(DPTQ_ERR_INVALID_ARG, bad == kDevBadPage ? "a KV8 call met a page number outside the cache"
+                                                       : "a KV8 call's sequence exceeded its declared tokens or length");
 }
 
 dptq_status dptq_scratch_buffers(void** ptrs, size_t* bytes, int* allocated, int max, int* count) {

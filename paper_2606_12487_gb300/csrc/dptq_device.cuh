@@ -77,7 +77,7 @@ enum DeviceError : int {
   kDevTimeoutDrain = 0x106,
   kDevTimeoutGrid = 0x107,     // grid-wide phase barrier did not complete
   kDevTimeoutRowMax = 0x108,   // a row's parts did not all post their maxima
-  // Contents of a KV8 call's device arrays that are out of range (not a wait).
+  // Contents of a KV8 call's device arrays that are out of range (not a wait; a word of its own).
   kDevBadBatch = 0x301,        // a sequence's tokens or length exceed what the call declared
   kDevBadPage = 0x302,         // a page number outside the cache
 };

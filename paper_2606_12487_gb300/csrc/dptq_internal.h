@@ -126,7 +126,8 @@ struct Kv8Args {
   int seqs, table_stride, tokens, max_tokens, max_len;
   int num_blocks, kv_heads, head_dim;
   int log2_page;         // tokens of a page: 16 to 128
-  int* err;              // device error word
+  int* err;              // device error word of waits that gave up
+  int* bad;              // and of arrays out of range, apart: neither hides the other
 };
 struct Kv8AppendArgs {
   Kv8Args c;

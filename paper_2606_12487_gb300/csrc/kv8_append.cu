@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(512, 3) kv8_append_pages_kernel(const Kv8Appen
     x[i] = ld_plain(reinterpret_cast<const uint4*>(src + row * a.stride) + (v & (vecs - 1)));
   }
   if (entry < 0 || entry >= c.num_blocks) {
-    atomicCAS(c.err, 0, kDevBadPage);
+    atomicCAS(c.bad, 0, kDevBadPage);
     return;
   }
   const size_t hb = (size_t)entry * c.kv_heads + head;

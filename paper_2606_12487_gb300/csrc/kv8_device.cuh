@@ -25,7 +25,7 @@ __device__ __forceinline__ bool load_seq(const Kv8Args& c, int s, Seq& q, bool t
   q.n = b - a;
   q.len = len;
   q.start = len - q.n;
-  if (!ok && tells) atomicCAS(c.err, 0, kDevBadBatch);
+  if (!ok && tells) atomicCAS(c.bad, 0, kDevBadBatch);
   return ok;
 }
 
@@ -34,7 +34,7 @@ __device__ __forceinline__ bool load_seq(const Kv8Args& c, int s, Seq& q, bool t
 __device__ __forceinline__ int load_page(const Kv8Args& c, int s, int page) {
   const int b = ld_plain(c.table + (long long)s * c.table_stride + page);
   if (b >= 0 && b < c.num_blocks) return b;
-  atomicCAS(c.err, 0, kDevBadPage);
+  atomicCAS(c.bad, 0, kDevBadPage);
   return -1;
 }
 

@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv8_prefill_kernel(const Kv8At
     auto checked = [&](int b) {
       if (b == kNoEntry) return -1;
       if (b >= 0 && b < c.num_blocks) return b;
-      atomicCAS(c.err, 0, kDevBadPage);
+      atomicCAS(c.bad, 0, kDevBadPage);
       return -1;
     };
     // (a page that is not there reads page 0: its keys have b = -inf below, and any codes do)

@@ -84,3 +84,56 @@ def test_a_wait_that_runs_out_ends_the_kernel(what):
     r = subprocess.run([sys.executable, "-c", textwrap.dedent(CHILD)], cwd=ROOT, env=env, capture_output=True, text=True,
                        timeout=300)
     assert r.returncode == 0 and "gave up and went on" in r.stdout, r.stdout + r.stderr
+
+
+BOTH = """
+import numpy as np, torch
+from paper_2606_12487_gb300 import dptq, inputs
+W = torch.from_numpy(inputs.weights(4096, 4096, layer=1)).cuda()
+x = torch.from_numpy(inputs.activations(inputs.llama2_7b_decode(), 32, 4096)).cuda()
+layer = dptq.dptq_pack_weights(W, 4096)
+y = torch.empty((32, 4096), dtype=torch.float16, device="cuda")
+cache = dptq.Kv8Cache.empty(4, 1, 16, 128)
+i32 = dict(dtype=torch.int32, device="cuda")
+def attend(n, page):
+    b = dptq.Kv8Batch(torch.tensor([0, n], **i32), torch.tensor([n], **i32), torch.full((1, 3), page, **i32),
+                      tokens=n, max_tokens=n, max_len=n)
+    q = torch.zeros((n, 1, 128), dtype=torch.float16, device="cuda")
+    dptq.dptq_kv8_attention(cache, b, q, q.clone(), 0.1)
+def answers(calls=3):
+    got = []
+    for _ in range(calls):
+        try:
+            dptq.dptq_last_device_error()
+            got.append(0)
+        except dptq.DptqError as e:
+            got.append(e.status)
+    return got
+attend(1, 9)                               # a bad page, then a prompt that gives up
+attend(33, 0)
+print(answers())
+attend(33, 9)                              # a bad page alone
+print(answers())
+attend(1, 9)                               # a bad page, then a GEMM that gives up
+dptq.dptq_qlinear(layer, x, 4, y)
+print(answers())
+attend(1, 9)
+ref = y.clone()
+dptq.dptq_qlinear(layer, x, 4, ref)        # (their order does not matter, and the GEMM's scratch is clean)
+print(answers(2))
+dptq.dptq_qlinear(layer, x, 4, y)
+print(answers(1), torch.equal(ref, y))
+"""
+
+
+@pytest.mark.gpu
+def test_a_bad_page_hides_no_wait_that_gave_up():
+    """Both are reported: first the time-out, whose call left its output incomplete, then the page."""
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    env = dict(os.environ, DPTQ_WAIT_CYCLES="200000", DPTQ_TEST_KV8_SHORTFALL="01", DPTQ_TEST_ROWS_SHORTFALL="1")
+    r = subprocess.run([sys.executable, "-c", textwrap.dedent(BOTH)], cwd=ROOT, env=env, capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+    assert r.stdout.split("\n")[:5] == ["[5, 1, 0]", "[1, 0, 0]", "[5, 1, 0]", "[1, 0]", "[0] True"], r.stdout
