@@ -188,7 +188,7 @@ dptq_status dptq_add_rmsnorm_quant(const void* x_fp16, const void* residual_fp16
 
 /* A paged KV cache of int8 codes with one fp32 scale for each page of tokens and KV head:
  * value = scale * code, scale >= 0.  Codes [num_blocks][kv_heads][block_tokens][head_dim], 16-byte aligned;
- * scales [num_blocks][kv_heads].  All device memory of the caller; the struct itself is host
+ * scales [num_blocks][kv_heads], like the batch's arrays 4-byte aligned.  All device memory of the caller; the struct itself is host
  * memory, read during the call only.  head_dim 64 or 128; block_tokens 16, 32, 64 or 128. */
 typedef struct dptq_kv8_cache {
   int8_t* k_codes;

@@ -531,6 +531,7 @@ dptq_status pack_weights_impl(const void* W_fp16, int N, int K, int had_block, c
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 }  // namespace
 
 dptq_status dptq_pack_weights(const void* W_fp16, int N, int K, int had_block, int w_on_device, dptq_handle* out) {
@@ -799,6 +800,9 @@ dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStre
     return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
   if (!aligned16(c->k_codes) || !aligned16(c->v_codes))
     return fail(DPTQ_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+  if (!aligned4(c->k_scales) || !aligned4(c->v_scales) || !aligned4(b->cu_tokens) || !aligned4(b->seq_lens) ||
+      !aligned4(b->block_table))
+    return fail(DPTQ_ERR_INVALID_ARG, "scales and the batch's arrays must be 4-byte aligned");
   if (b->max_len > (long long)b->table_stride * c->block_tokens)
     return fail(DPTQ_ERR_INVALID_ARG, "max_len exceeds the block table");
   int dev;

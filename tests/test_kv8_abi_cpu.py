@@ -106,3 +106,15 @@ def test_kv8_refuses_what_its_indexes_do_not_hold(dp, batch):
     cp, bp = ctypes.addressof(c), ctypes.addressof(b)
     assert lib.dptq_kv8_append(cp, bp, P(64), P(64), 256, None) == 2
     assert lib.dptq_kv8_attention(cp, bp, P(64), 1024, 8, F(0.1), 0, 0, P(64), 1024, None) == 2
+
+
+@pytest.mark.parametrize("cache,batch", [(dict(k_scales=66), {}), (dict(v_scales=65), {}), ({}, dict(cu_tokens=66)),
+                                         ({}, dict(seq_lens=67)), ({}, dict(block_table=66))])
+def test_kv8_refuses_misaligned_scales_and_arrays(dp, cache, batch):
+    """4-byte values that the kernels read whole: a misaligned read would fault."""
+    c, b = _handles(dp, cache, batch)
+    lib = dp.load()
+    cp, bp = ctypes.addressof(c), ctypes.addressof(b)
+    assert lib.dptq_kv8_append(cp, bp, P(64), P(64), 256, None) == 1
+    assert lib.dptq_kv8_attention(cp, bp, P(64), 1024, 8, F(0.1), 0, 0, P(64), 1024, None) == 1
+    assert b"aligned" in lib.dptq_last_error_message()
