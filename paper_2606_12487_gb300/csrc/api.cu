@@ -1,6 +1,7 @@
 // api.cu -- the C ABI of include/dptq.h: argument checks, the layer handle, the
-// per-device scratch, and the launch sequence of each call.  No compute happens here;
-// every step of the path runs in the kernels of rotate_quant.cu and qgemm.cu.
+// per-device scratch, and the launch sequence of each call.  No compute happens here: the
+// kernels are in rotate_quant.cu and qgemm.cu (the linear layer), kv_policy.cu (KV4, the
+// policy), norm_quant.cu and kv8_*.cu (the operators around the layer).
 #include <cmath>
 #include <cstdint>
 #include <algorithm>

@@ -2,7 +2,7 @@
 // paged int8 cache: decode steps and a few speculative tokens.
 //
 // The call is a stream over the visible K and V codes (one byte a value, read once) with
-// 4 R multiply-adds a byte pair for R rows, so bytes bound it.  Work is cut into steps of 32
+// 2 R multiply-adds (4 R flops) a pair of bytes for R rows, so bytes bound it.  Work is cut into steps of 32
 // keys of one (sequence, KV head); the CTAs of one resident wave take equal, contiguous
 // shares of all steps whatever the lengths are (they are read from the device), and a
 // (sequence, head) that several CTAs share is joined by the last of them to finish.
@@ -26,8 +26,9 @@
 // the second product are then p_j sv_j relative to the largest of them, and binary16 loses
 // nothing to pages whose scales are far apart; the denominator takes each back by 1 / sv.
 //
-// 32 ragged sequences up to 4096 tokens, 32 heads of 128 (579 MB): 98.6 us, 5.9 TB/s; one of 131072 tokens,
-// 64 over 8 heads (269 MB): 54.9 us, 4.9 TB/s, of which the join of 57 shares a head takes about 6.
+// 32 ragged sequences up to 4096 tokens, 32 heads of 128 (579 MB): 98.7 us, 5.9 TB/s (of 64, 289 MB: 68.0 us,
+// 4.3 TB/s); one of 131072 tokens, 64 over 8 heads (269 MB): 54.9 us, 4.9 TB/s, of which the join of 57 shares a
+// head takes about 6.
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
@@ -38,8 +39,8 @@ namespace dptq {
 
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
 constexpr int kDecKeys = 32;        // keys of a step
-// Fewest steps that a CTA is started for: one a warp (one sequence of 512 tokens, 8 heads: 9.4 us; 8 steps:
-// 10.6 us).  Most partial results joined at once (57 of one sequence of 131072 tokens in two levels: 54.9 us;
+// Fewest steps that a CTA is started for: one a warp (one sequence, 8 heads, with 4 / 8 steps, us: of 512 tokens
+// 9.5 / 10.1, of 2048 12.8 / 10.9, of 8192 13.5 / 16.6).  Most partial results joined at once (57 of one sequence of 131072 tokens in two levels: 54.9 us;
 // in one: 59.3 us), and of a group, or groups: sqrt of a grid of 1024 CTAs at most.
 constexpr int kDecMinSteps = 4, kDecJoin = 12, kDecJoinMost = 32;
 
@@ -60,7 +61,9 @@ __device__ __forceinline__ void widen_pairs(uint32_t a, uint32_t b, uint32_t (&r
 }
 // What a (sequence, head) costs a CTA beyond its steps (its rows of q, the first copies' latency,
 // the join): shares of 16 steps and more are cut as if every one had so many steps more, which
-// come first.  32 ragged MHA sequences (7 to 128 steps a head): 124 us without, 100 us with 6 or 10.
+// come first.  With 6 / without, us: 32 ragged MHA sequences (7 to 128 steps a head) 98.8 / 121.0, the same with heads
+// of 64 68.0 / 88.2, 64 with a window over 8 heads 90.4 / 95.0, 16 up to 8000 tokens over 8 heads 39.0 / 40.9, 64
+// of 8000 tokens over 8 heads, two rows each, 210 / 208 (equal lengths).
 constexpr int kDecExtra = 6, kDecExtraFrom = 16;
 
 // The steps of a sequence: `sink` steps from key 0, then steps from key `from`.
@@ -81,8 +84,8 @@ __device__ __forceinline__ Steps seq_steps(const Seq& q, int window, int sinks) 
   return r;
 }
 
-// Steps of sequences 0 .. s - 1 (of one head each): the CTA sums them chunk by chunk.
-__device__ __forceinline__ int block_scan(int v, int* red, int& total) {   // exclusive prefix over the CTA's threads
+// The exclusive prefix of v over the CTA's threads, and its sum over all of them.
+__device__ __forceinline__ int block_scan(int v, int* red, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = v;
 #pragma unroll

@@ -20,13 +20,14 @@
 // tiles are split along the keys: each CTA leaves its rows' sums, and a second launch joins
 // them.
 //
-// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 808 us, 1361
+// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 811 us, 1356
 // TFLOP/s, 71 % of the measured bf16 rate): the chain of a row tile from S over its softmax
 // (about 2400 cycles, two tiles taking turns) back to the next S.  Without the softmax's
 // waits the MMAs and the widening take 605 us (pairs; 720 us for CTAs alone, which are short of
-// shared-memory bandwidth: q, K and V tiles are read at its full rate by the MMAs).  The roles'
-// code has to stay short: they fetch it from one instruction cache (rolled loops and rare code
-// apart: 1041 -> 904 and 878 -> 817 us).
+// shared-memory bandwidth: q, K and V tiles are read at its full rate by the MMAs).  The same prompt with
+// heads of 64, which take no pairs: 705 us; 256 rows behind 16000 tokens, 8 over one head, split along
+// the keys, with the join: 38 us.  The roles' code has to stay short: they fetch it from one
+// instruction cache (rolled loops and rare code apart: 1041 -> 904 and 878 -> 817 us).
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
@@ -736,9 +737,11 @@ __global__ void __launch_bounds__(256) kv8_join_kernel(const Kv8AttendArgs A, in
 }
 
 // Rows of a sequence and KV head from which pairs of CTAs take them.  Pairs / CTAs alone, us, 64 over 8
-// heads: 16 sequences x 64 new tokens behind 4000: 118 / 133; 16 x 256: 363 / 399; 1 x 2048 behind 8000:
-// 464 / 526; 2 x 4096: 357 / 383; 4 x 1024: 83 / 80.  Pairs lose where sequences of one or two pair tiles
-// round up into another wave: 16 x about 100 behind 4000: 228 / 200.
+// heads: 16 sequences x 64 new tokens behind 4000: 119 / 133; 16 x 256: 369 / 405; 4 x 1024: 382 / 429;
+// 1 x 2048 behind 8000: 471 / 549; 2 x 4096: 364 / 391; 1 x 8192: 811 / 898; 32 over 8 heads, 8 x 512 behind up to
+// 4000: 173 / 187.  Pairs lose where sequences of one or two pair tiles round up into another wave (16 x
+// about 100 behind 4000: 220 / 200) and where rows without a context see few tiles each (4 x 1024: 85 / 81;
+// 32 heads, 8 x 512: 61 / 46): long sums, which pairs serve, weigh more than the start of short ones.
 constexpr int kPairRows = 512;
 
 template <int D>

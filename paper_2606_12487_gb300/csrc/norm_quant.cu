@@ -12,9 +12,10 @@
 // registers a thread), so that one's loads run under another's reduction, and a call of few
 // tokens is as long as its chain of one load, one reduction and one store.  Tokens that
 // registers do not hold (K > 16384) are read again from the second-level cache.
-// 8192 x 8192 (470 MB): 71 us, 6.6 TB/s.  CTAs of 1024 threads: 92 us; three of 512 an SM: 86 us; a
-// resident wave of CTAs that ask for their next token before they reduce this one: 100 us (the
-// second token's registers cost a resident CTA and more).
+// 8192 x 8192 (470 MB): 71 us, 6.6 TB/s (4-bit codes, 436 MB: 70 us); 2048 x 28672 (411 MB and a second
+// read): 111 us.  At 8192 x 8192, CTAs of 1024 threads: 92 us; three of 512 an SM: 86 us; a resident wave of
+// CTAs that ask for their next token before they reduce this one: 100 us (the second token's
+// registers cost a resident CTA and more).
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
