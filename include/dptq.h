@@ -258,9 +258,99 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
                                long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
                                long long out_stride, void* stream);
 
-/* Allocate the scratch of the two calls above on the current device, so that neither allocates
- * (for example before a stream capture).  Synchronous. */
+/* Allocate the scratch of the two calls above, and of the rotary and 4-bit cache calls below, on the current
+ * device, so that none of them allocates (for example before a stream capture).  Synchronous. */
 dptq_status dptq_kv8_reserve(void);
+
+/* ---- Rotary positions, and the 4-bit KV cache (Section 4.2, Algorithm 1 steps 1 and 4: symmetric, groups
+ * along the head dimension, here one group a token and head) with its attention.  The batch is the one above. */
+
+/* A paged KV cache of 4-bit codes with one scale for each token and KV head.  Codes uint8
+ * [num_blocks][kv_heads][block_tokens][head_dim / 2] in the nibble format of
+ * dptq_kv4_quantize (two's complement, low nibble = even dim); scales bfloat16 (raw bits)
+ * [num_blocks][kv_heads][block_tokens].  Codes and scales 16-byte aligned.  A cached value is
+ * binary16(scale * code), which is exact for scales of 2^-17 and more (8 + 3 significant bits): the tensor
+ * cores, the read-back and the definition below all see the same values.  head_dim 64 or 128;
+ * block_tokens 16, 32, 64 or 128.  All device memory of the caller; the struct is read during the call only. */
+typedef struct dptq_kv4_cache {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  uint16_t* k_scales;
+  uint16_t* v_scales;
+  int num_blocks, kv_heads, block_tokens, head_dim;
+} dptq_kv4_cache;
+
+/* Quantize the K and V rows of new tokens into the cache, each token and head on its own:
+ *   scale = bfloat16(max|x| * fl(1 / 7)), rounded to nearest even;  code = round-half-even(x / scale), the IEEE
+ *   fp32 quotient;  scale 0 gives codes 0.
+ * Codes are in [-7, 7].  A NaN counts for nothing in the maximum and takes the code 0; a row with an
+ * infinite value has an infinite scale and codes 0.  Earlier tokens of a page are not touched.
+ * A position is written by one row of the batch at most.  Arguments, rows and errors as dptq_kv8_append. */
+dptq_status dptq_kv4_append(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
+                            const void* v_fp16, long long token_stride, void* stream);
+
+/* The cached values of the batch's rows, binary16(scale * code): row i of a sequence's n gets the K and V
+ * heads of position seq_lens - n + i (rows of the whole sequence: cu_tokens with n = seq_lens).
+ * k_out, v_out: device rows of `tokens` tokens, kv_heads * head_dim binary16 values each, token_stride
+ * elements apart; 16-byte aligned, token_stride a multiple of 8.  Rows at negative positions, and rows whose
+ * page is out of range (INVALID_ARG from dptq_last_device_error), are left as they are.  A scale that is
+ * infinite or NaN gives infinities and NaN as the product has them.  Errors as dptq_kv8_append. */
+dptq_status dptq_kv4_read(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, void* k_out, void* v_out,
+                          long long token_stride, void* stream);
+
+/* Causal attention of the batch's rows over the 4-bit cache, query head h reading KV head
+ * h / (q_heads / kv_heads):
+ *   out = sum_j softmax(scale * q . k_j)_j v_j  over the keys j that the query sees,
+ * as dptq_kv8_attention defines them (window, sinks, zeros for a query that sees none).  A query that sees a key
+ * whose K or V scale is infinite or NaN gets NaN; no other query is touched by it, and NaN in q
+ * stays in its row.  Logits, maxima, sums and accumulators are fp32; softmax weights are rounded to binary16
+ * relative to their largest so far.
+ * Uses the scratch of dptq_kv8_attention (dptq_kv8_reserve allocates it).  Arguments and errors as there. */
+dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
+                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
+                               long long out_stride, void* stream);
+
+/* The angles per position (radians) of rotary pairs, HOST arrays of rot_dim / 2 doubles:
+ * f_i = base^(-2 i / rot_dim), changed for contexts longer than the trained ones by `scaling`:
+ *   NONE        f_i
+ *   LINEAR      f_i / factor
+ *   NTK         f_i of base * factor^(rot_dim / (rot_dim - 2))
+ *   WAVELENGTH  k f_i + (1 - k) f_i / factor, k = (t_i - low) / (high - low) clamped to [0, 1],
+ *               t_i = trained_len f_i / 2 pi the turns of pair i in the trained length
+ *   RAMP        the same with k = 1 - (i - a) / max(b - a, 0.001) clamped, a = floor(d(high)) but not below 0,
+ *               b = ceil(d(low)) but not above rot_dim - 1, d(t) the i at which t_i = t.
+ * rot_dim even and >= 2 (NTK: >= 4); base > 1; factor > 0; for the last two trained_len > 0 and
+ * 0 < low < high.  Arguments that `scaling` does not use are not looked at.  Host only.  INVALID_ARG otherwise. */
+#define DPTQ_ROTARY_NONE 0
+#define DPTQ_ROTARY_LINEAR 1
+#define DPTQ_ROTARY_NTK 2
+#define DPTQ_ROTARY_WAVELENGTH 3
+#define DPTQ_ROTARY_RAMP 4
+dptq_status dptq_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double trained_len, double low,
+                                    double high, double* freq);
+
+/* Angles per position as 64-bit fractions of a turn: turns[i] = round(frac(freq[i] / 2 pi) 2^64) mod 2^64.  A
+ * position times them is exact modulo whole turns, so the angle of any position is good to 2^-53 of
+ * itself or 2^-64 turns a position.  Negative frequencies turn the other way.  HOST arrays of n
+ * values.  INVALID_ARG for null pointers, n < 0 and frequencies that are not finite. */
+dptq_status dptq_rotary_turns(const double* freq, int n, uint64_t* turns);
+
+/* Rotary positions: the first rot_dim values of every head are rot_dim / 2 pairs (x1, x2), values i and
+ * i + rot_dim / 2 (interleaved = 0) or 2 i and 2 i + 1 (interleaved = 1), and pair i of the row at position p,
+ * with theta = 2 pi frac(p turns[i] / 2^64), becomes
+ *   amplitude (x1 cos - x2 sin, x1 sin + x2 cos),
+ * in fp32 from correctly reduced angles, rounded to binary16 once.  Positions are the batch's (its table is not looked
+ * at and may be NULL); rows at negative positions and outside of its sequences are left as they are.
+ * x_fp16, out_fp16: device rows of `tokens` tokens, heads * head_dim binary16 values each, x_stride / out_stride
+ * elements apart; 16-byte aligned, strides multiples of 8.  out_fp16 may be x_fp16 itself with the same
+ * stride, else the two may not overlap; the rest of a head is copied.  turns: device [rot_dim / 2], 8-byte aligned.
+ * head_dim: a multiple of 8 up to 512; rot_dim even, 2 to head_dim; heads 1 to 65535.
+ * Asynchronous.  INVALID_ARG for null or misaligned pointers and bad sizes; UNSUPPORTED for sizes beyond these and
+ * those of dptq_kv8_append.  seqs == 0 or tokens == 0 is a no-op.  The first call on a device allocates as
+ * there. */
+dptq_status dptq_rotary(const dptq_kv8_batch* batch, const void* x_fp16, long long x_stride, int heads, int head_dim,
+                        const uint64_t* turns, int rot_dim, int interleaved, float amplitude, void* out_fp16,
+                        long long out_stride, void* stream);
 
 /* The quantized linear layer: out = fp16( Q(x R) (W R)^T scaled ), i.e. rotate and
  * quantize x with `bits` (4 or 8, the layer's mask entry), multiply by the packed

@@ -1,7 +1,7 @@
 // api.cu -- the C ABI of include/dptq.h: argument checks, the layer handle, the
 // per-device scratch, and the launch sequence of each call.  No compute happens here: the
 // kernels are in rotate_quant.cu and qgemm.cu (the linear layer), kv_policy.cu (KV4, the
-// policy), norm_quant.cu and kv8_*.cu (the operators around the layer).
+// policy), norm_quant.cu, rotary.cu, kv8_*.cu and kv4_*.cu (the operators around the layer).
 #include <cmath>
 #include <cstdint>
 #include <algorithm>
@@ -413,7 +413,7 @@ int take_rows_shortfall() {
   return left.exchange(0);
 }
 
-// DPTQ_TEST_KV8_SHORTFALL=abc: the digits, one for each call of dptq_kv8_attention.
+// DPTQ_TEST_KV8_SHORTFALL=abc: the digits, one for each call of dptq_kv8_attention or dptq_kv4_attention.
 int take_kv8_shortfall() {
   static const char* const v = std::getenv("DPTQ_TEST_KV8_SHORTFALL");
   if (v == nullptr) return 0;
@@ -778,43 +778,26 @@ dptq_status dptq_sensitivity_policy(const float* x, const float* dx, int L, int 
 }
 
 namespace {
-// The host's part of a KV8 call's checks; *none: nothing to do.
-dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStream_t s, Kv8Args* a, bool* none,
-                      Scratch** sc) {
-  *none = false;
-  if (!c || !b) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
-  if (c->num_blocks <= 0 || c->kv_heads <= 0 || c->block_tokens <= 0 || c->head_dim <= 0)
-    return fail(DPTQ_ERR_INVALID_ARG, "bad cache sizes");
+// The bounds of a batch; *none: nothing to do.
+dptq_status check_batch_sizes(const dptq_kv8_batch* b) {
   if (b->seqs < 0 || b->tokens < 0 || b->max_tokens < 0 || b->max_len < 0 || b->table_stride < 0)
     return fail(DPTQ_ERR_INVALID_ARG, "bad batch sizes");
-  if (c->head_dim != 64 && c->head_dim != 128) return fail(DPTQ_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
-  if (c->block_tokens < 16 || c->block_tokens > 128 || !is_pow2(c->block_tokens))
-    return fail(DPTQ_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
-  if (c->kv_heads > 1023 || b->seqs > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "too many heads or sequences");
+  return DPTQ_OK;
+}
+dptq_status check_batch_limits(const dptq_kv8_batch* b, bool* none) {
+  if (b->seqs > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "too many heads or sequences");
   if (b->max_tokens > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "more than 65535 rows of a sequence in one call");
   if (b->max_len > 1 << 27) return fail(DPTQ_ERR_UNSUPPORTED, "sequences longer than 2^27 tokens");
-  if (b->seqs == 0 || b->tokens == 0 || b->max_tokens == 0) {
-    *none = true;
-    return DPTQ_OK;
-  }
-  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !b->cu_tokens || !b->seq_lens || !b->block_table)
-    return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
-  if (!aligned16(c->k_codes) || !aligned16(c->v_codes))
-    return fail(DPTQ_ERR_INVALID_ARG, "codes must be 16-byte aligned");
-  if (!aligned4(c->k_scales) || !aligned4(c->v_scales) || !aligned4(b->cu_tokens) || !aligned4(b->seq_lens) ||
-      !aligned4(b->block_table))
-    return fail(DPTQ_ERR_INVALID_ARG, "scales and the batch's arrays must be 4-byte aligned");
-  if (b->max_len > (long long)b->table_stride * c->block_tokens)
-    return fail(DPTQ_ERR_INVALID_ARG, "max_len exceeds the block table");
+  *none = b->seqs == 0 || b->tokens == 0 || b->max_tokens == 0;
+  return DPTQ_OK;
+}
+// The kernels' view of a batch, and the device's scratch (its error words).
+dptq_status take_batch(const dptq_kv8_batch* b, cudaStream_t s, Kv8Args* a, Scratch** sc) {
   int dev;
   dptq_status st = current_device(&dev);
   if (st != DPTQ_OK) return st;
   if ((st = ensure_scratch(dev, 0, 0, s, sc)) != DPTQ_OK) return st;
   *a = Kv8Args{};
-  a->codes[0] = c->k_codes;
-  a->codes[1] = c->v_codes;
-  a->scales[0] = c->k_scales;
-  a->scales[1] = c->v_scales;
   a->cu = b->cu_tokens;
   a->lens = b->seq_lens;
   a->table = b->block_table;
@@ -823,12 +806,63 @@ dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStre
   a->tokens = b->tokens;
   a->max_tokens = std::min(b->max_tokens, b->tokens);
   a->max_len = b->max_len;
+  a->err = (*sc)->err;
+  a->bad = (*sc)->err + 1;
+  return DPTQ_OK;
+}
+
+// The host's part of the checks of a call on a paged cache (Cache: dptq_kv8_cache or dptq_kv4_cache, whose
+// scales are of `scale_bytes`); *none: nothing to do.
+extern "C++" template <class Cache>
+dptq_status check_paged(const Cache* c, const dptq_kv8_batch* b, unsigned scale_bytes, cudaStream_t s, Kv8Args* a,
+                        bool* none, Scratch** sc) {
+  *none = false;
+  if (!c || !b) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (c->num_blocks <= 0 || c->kv_heads <= 0 || c->block_tokens <= 0 || c->head_dim <= 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "bad cache sizes");
+  dptq_status st = check_batch_sizes(b);
+  if (st != DPTQ_OK) return st;
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(DPTQ_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (c->block_tokens < 16 || c->block_tokens > 128 || !is_pow2(c->block_tokens))
+    return fail(DPTQ_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
+  if (c->kv_heads > 1023) return fail(DPTQ_ERR_UNSUPPORTED, "too many heads or sequences");
+  if ((st = check_batch_limits(b, none)) != DPTQ_OK || *none) return st;
+  if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales || !b->cu_tokens || !b->seq_lens || !b->block_table)
+    return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes))
+    return fail(DPTQ_ERR_INVALID_ARG, "codes must be 16-byte aligned");
+  const uintptr_t scales = reinterpret_cast<uintptr_t>(c->k_scales) | reinterpret_cast<uintptr_t>(c->v_scales);
+  if ((scales & (scale_bytes - 1)) != 0 || !aligned4(b->cu_tokens) || !aligned4(b->seq_lens) || !aligned4(b->block_table))
+    return fail(DPTQ_ERR_INVALID_ARG,
+                "scales must be " + std::to_string(scale_bytes) + "-byte aligned, the batch's arrays 4-byte aligned");
+  if (b->max_len > (long long)b->table_stride * c->block_tokens)
+    return fail(DPTQ_ERR_INVALID_ARG, "max_len exceeds the block table");
+  if ((st = take_batch(b, s, a, sc)) != DPTQ_OK) return st;
   a->num_blocks = c->num_blocks;
   a->kv_heads = c->kv_heads;
   a->head_dim = c->head_dim;
   a->log2_page = c->block_tokens == 16 ? 4 : c->block_tokens == 32 ? 5 : c->block_tokens == 64 ? 6 : 7;
-  a->err = (*sc)->err;
-  a->bad = (*sc)->err + 1;
+  return DPTQ_OK;
+}
+dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStream_t s, Kv8Args* a, bool* none,
+                      Scratch** sc) {
+  const dptq_status st = check_paged(c, b, 4, s, a, none, sc);
+  if (st != DPTQ_OK || *none) return st;
+  a->codes[0] = c->k_codes;
+  a->codes[1] = c->v_codes;
+  a->scales[0] = c->k_scales;
+  a->scales[1] = c->v_scales;
+  return DPTQ_OK;
+}
+dptq_status check_kv4(const dptq_kv4_cache* c, const dptq_kv8_batch* b, cudaStream_t s, Kv4Args* a, bool* none,
+                      Scratch** sc) {
+  // (16 scales of a page's tokens are read at a time)
+  const dptq_status st = check_paged(c, b, 16, s, &a->c, none, sc);
+  if (st != DPTQ_OK || *none) return st;
+  a->codes[0] = c->k_codes;
+  a->codes[1] = c->v_codes;
+  a->scales[0] = c->k_scales;
+  a->scales[1] = c->v_scales;
   return DPTQ_OK;
 }
 
@@ -860,30 +894,30 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
   return DPTQ_OK;
 }
 
-dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
-                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
-                               long long out_stride, void* stream) {
-  NvtxRange nvtx_range("dptq_kv8_attention");
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
+namespace {
+dptq_status check_attention(int q_heads, int kv_heads, float scale, int window, int sinks) {
   if (q_heads <= 0 || window < 0 || sinks < 0 || !std::isfinite(scale))
     return fail(DPTQ_ERR_INVALID_ARG, "bad q_heads, window, sinks or scale");
-  if (cache && cache->kv_heads > 0) {
-    if (q_heads % cache->kv_heads != 0) return fail(DPTQ_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
-    if (q_heads / cache->kv_heads > 64) return fail(DPTQ_ERR_UNSUPPORTED, "more than 64 query heads for a KV head");
+  if (kv_heads > 0) {
+    if (q_heads % kv_heads != 0) return fail(DPTQ_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
+    if (q_heads / kv_heads > 64) return fail(DPTQ_ERR_UNSUPPORTED, "more than 64 query heads for a KV head");
   }
-  Kv8AttendArgs a{};
-  Scratch* sc = nullptr;
-  bool none;
-  dptq_status st = check_kv8(cache, batch, s, &a.c, &none, &sc);
-  if (st != DPTQ_OK || none) return st;
-  if ((st = check_rows(q_fp16, q_stride, q_heads, cache->head_dim)) != DPTQ_OK) return st;
-  if ((st = check_rows(out_fp16, out_stride, q_heads, cache->head_dim)) != DPTQ_OK) return st;
+  return DPTQ_OK;
+}
+// The rows, masks and scratch of an attention call.
+extern "C++" template <class Args>
+dptq_status fill_attention(Args& a, Scratch* sc, cudaStream_t s, const dptq_kv8_batch* batch, int kv_heads, int head_dim,
+                           const void* q_fp16, long long q_stride, int q_heads, float scale, int window, int sinks,
+                           void* out_fp16, long long out_stride) {
+  dptq_status st;
+  if ((st = check_rows(q_fp16, q_stride, q_heads, head_dim)) != DPTQ_OK) return st;
+  if ((st = check_rows(out_fp16, out_stride, q_heads, head_dim)) != DPTQ_OK) return st;
   a.q = static_cast<const __half*>(q_fp16);
   a.out = static_cast<__half*>(out_fp16);
   a.q_stride = q_stride;
   a.out_stride = out_stride;
   a.q_heads = q_heads;
-  a.group = q_heads / cache->kv_heads;
+  a.group = q_heads / kv_heads;
   a.scale = scale;
   a.window = window < batch->max_len ? window : 0;   // (a window that holds every position)
   a.sinks = std::min(sinks, batch->max_len);
@@ -892,8 +926,163 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
   a.counters = sc->kv8_counters;
   a.wait_cycles = wait_cycles_setting();
   a.shortfall = take_kv8_shortfall();
+  return DPTQ_OK;
+}
+}  // namespace
+
+dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
+                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
+                               long long out_stride, void* stream) {
+  NvtxRange nvtx_range("dptq_kv8_attention");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  dptq_status st = check_attention(q_heads, cache ? cache->kv_heads : 0, scale, window, sinks);
+  if (st != DPTQ_OK) return st;
+  Kv8AttendArgs a{};
+  Scratch* sc = nullptr;
+  bool none;
+  st = check_kv8(cache, batch, s, &a.c, &none, &sc);
+  if (st != DPTQ_OK || none) return st;
+  if ((st = fill_attention(a, sc, s, batch, cache->kv_heads, cache->head_dim, q_fp16, q_stride, q_heads, scale, window,
+                           sinks, out_fp16, out_stride)) != DPTQ_OK)
+    return st;
   const bool decode = (long long)a.c.max_tokens * a.group <= kDecodeRows;
   DPTQ_CUDA(decode ? launch_kv8_decode(a, sc->num_sms, s) : launch_kv8_prefill(a, sc->num_sms, s), "kv8_attention launch");
+  return DPTQ_OK;
+}
+
+namespace {
+dptq_status kv4_rows(const char* what, const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* k,
+                     const void* v, long long stride, void* stream,
+                     cudaError_t (*launch)(const Kv4RowsArgs&, int, cudaStream_t)) {
+  NvtxRange nvtx_range(what);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Kv4RowsArgs a{};
+  Scratch* sc = nullptr;
+  bool none;
+  dptq_status st = check_kv4(cache, batch, s, &a.k, &none, &sc);
+  if (st != DPTQ_OK || none) return st;
+  if ((st = check_rows(k, stride, cache->kv_heads, cache->head_dim)) != DPTQ_OK) return st;
+  if ((st = check_rows(v, stride, cache->kv_heads, cache->head_dim)) != DPTQ_OK) return st;
+  a.rows[0] = static_cast<__half*>(const_cast<void*>(k));
+  a.rows[1] = static_cast<__half*>(const_cast<void*>(v));
+  a.stride = stride;
+  DPTQ_CUDA(launch(a, sc->num_sms, s), what);
+  return DPTQ_OK;
+}
+}  // namespace
+
+dptq_status dptq_kv4_append(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
+                            const void* v_fp16, long long token_stride, void* stream) {
+  return kv4_rows("dptq_kv4_append", cache, batch, k_fp16, v_fp16, token_stride, stream, launch_kv4_append);
+}
+
+dptq_status dptq_kv4_read(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, void* k_out, void* v_out,
+                          long long token_stride, void* stream) {
+  return kv4_rows("dptq_kv4_read", cache, batch, k_out, v_out, token_stride, stream, launch_kv4_read);
+}
+
+dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
+                               long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,
+                               long long out_stride, void* stream) {
+  NvtxRange nvtx_range("dptq_kv4_attention");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  dptq_status st = check_attention(q_heads, cache ? cache->kv_heads : 0, scale, window, sinks);
+  if (st != DPTQ_OK) return st;
+  Kv4AttendArgs a{};
+  Scratch* sc = nullptr;
+  bool none;
+  st = check_kv4(cache, batch, s, &a.k, &none, &sc);
+  if (st != DPTQ_OK || none) return st;
+  if ((st = fill_attention(a, sc, s, batch, cache->kv_heads, cache->head_dim, q_fp16, q_stride, q_heads, scale, window,
+                           sinks, out_fp16, out_stride)) != DPTQ_OK)
+    return st;
+  DPTQ_CUDA(launch_kv4_decode(a, sc->num_sms, s), "kv4_attention launch");
+  return DPTQ_OK;
+}
+
+dptq_status dptq_rotary_frequencies(int rot_dim, double base, int scaling, double factor, double trained_len, double low,
+                                    double high, double* freq) {
+  if (!freq) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (rot_dim < 2 || rot_dim % 2 != 0) return fail(DPTQ_ERR_INVALID_ARG, "rot_dim must be even and at least 2");
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(DPTQ_ERR_INVALID_ARG, "base must be finite and above 1");
+  if (scaling < DPTQ_ROTARY_NONE || scaling > DPTQ_ROTARY_RAMP) return fail(DPTQ_ERR_INVALID_ARG, "unknown scaling");
+  if (scaling != DPTQ_ROTARY_NONE && (!(factor > 0.0) || !std::isfinite(factor)))
+    return fail(DPTQ_ERR_INVALID_ARG, "factor must be finite and above 0");
+  if (scaling == DPTQ_ROTARY_NTK) {
+    if (rot_dim < 4) return fail(DPTQ_ERR_INVALID_ARG, "NTK scaling takes a rot_dim of at least 4");
+    base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+  }
+  const bool by_turns = scaling == DPTQ_ROTARY_WAVELENGTH || scaling == DPTQ_ROTARY_RAMP;
+  if (by_turns && !(trained_len > 0.0 && std::isfinite(trained_len) && low > 0.0 && low < high && std::isfinite(high)))
+    return fail(DPTQ_ERR_INVALID_ARG, "trained_len must be above 0 and 0 < low < high");
+  constexpr double kTwoPi = 6.283185307179586476925;
+  double a = 0.0, b = 0.0;
+  if (scaling == DPTQ_ROTARY_RAMP) {
+    auto dim = [&](double turns) { return rot_dim * std::log(trained_len / (kTwoPi * turns)) / (2.0 * std::log(base)); };
+    a = std::max(std::floor(dim(high)), 0.0);
+    b = std::min(std::ceil(dim(low)), rot_dim - 1.0);
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / rot_dim);
+    double keep = 1.0;
+    if (scaling == DPTQ_ROTARY_LINEAR) keep = 0.0;
+    if (scaling == DPTQ_ROTARY_WAVELENGTH) keep = (trained_len * f / kTwoPi - low) / (high - low);
+    if (scaling == DPTQ_ROTARY_RAMP) keep = 1.0 - (i - a) / std::max(b - a, 0.001);
+    keep = std::min(std::max(keep, 0.0), 1.0);
+    freq[i] = keep == 1.0 ? f : keep * f + (1.0 - keep) * f / factor;
+  }
+  return DPTQ_OK;
+}
+
+dptq_status dptq_rotary_turns(const double* freq, int n, uint64_t* turns) {
+  if (n < 0 || (n > 0 && (!freq || !turns))) return fail(DPTQ_ERR_INVALID_ARG, "null pointer or negative size");
+  for (int i = 0; i < n; ++i)
+    if (!std::isfinite(freq[i])) return fail(DPTQ_ERR_INVALID_ARG, "a frequency is not finite");
+  constexpr double kPerTurn = 0.159154943091895335769;   // 1 / 2 pi
+  for (int i = 0; i < n; ++i) {
+    const double t = std::fabs(freq[i]) * kPerTurn;
+    const uint64_t u = static_cast<uint64_t>(std::rint(std::ldexp(t - std::floor(t), 64)));   // (at most 2^64 - 2^11)
+    turns[i] = freq[i] < 0.0 ? ~u + 1u : u;
+  }
+  return DPTQ_OK;
+}
+
+dptq_status dptq_rotary(const dptq_kv8_batch* batch, const void* x_fp16, long long x_stride, int heads, int head_dim,
+                        const uint64_t* turns, int rot_dim, int interleaved, float amplitude, void* out_fp16,
+                        long long out_stride, void* stream) {
+  NvtxRange nvtx_range("dptq_rotary");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (!batch) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  dptq_status st = check_batch_sizes(batch);
+  if (st != DPTQ_OK) return st;
+  if (heads <= 0 || head_dim <= 0 || rot_dim < 2 || rot_dim > head_dim || rot_dim % 2 != 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "bad heads, head_dim or rot_dim");
+  if (!std::isfinite(amplitude)) return fail(DPTQ_ERR_INVALID_ARG, "amplitude must be finite");
+  if (head_dim % 8 != 0 || head_dim > 512) return fail(DPTQ_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 up to 512");
+  if (heads > 65535) return fail(DPTQ_ERR_UNSUPPORTED, "more than 65535 heads");
+  bool none;
+  if ((st = check_batch_limits(batch, &none)) != DPTQ_OK || none) return st;
+  if (!batch->cu_tokens || !batch->seq_lens || !turns) return fail(DPTQ_ERR_INVALID_ARG, "null pointer");
+  if (!aligned4(batch->cu_tokens) || !aligned4(batch->seq_lens) || (reinterpret_cast<uintptr_t>(turns) & 7u) != 0)
+    return fail(DPTQ_ERR_INVALID_ARG, "the batch's arrays must be 4-byte aligned, turns 8-byte aligned");
+  if ((st = check_rows(x_fp16, x_stride, heads, head_dim)) != DPTQ_OK) return st;
+  if ((st = check_rows(out_fp16, out_stride, heads, head_dim)) != DPTQ_OK) return st;
+  if (x_fp16 == out_fp16 && x_stride != out_stride && batch->tokens > 1)
+    return fail(DPTQ_ERR_INVALID_ARG, "in place both strides are the same");
+  RotaryArgs a{};
+  Scratch* sc = nullptr;
+  if ((st = take_batch(batch, s, &a.c, &sc)) != DPTQ_OK) return st;
+  a.x = static_cast<const __half*>(x_fp16);
+  a.out = static_cast<__half*>(out_fp16);
+  a.turns = turns;
+  a.x_stride = x_stride;
+  a.out_stride = out_stride;
+  a.heads = heads;
+  a.head_dim = head_dim;
+  a.rot = rot_dim;
+  a.interleaved = interleaved != 0;
+  a.amplitude = amplitude;
+  DPTQ_CUDA(launch_rotary(a, sc->num_sms, s), "rotary launch");
   return DPTQ_OK;
 }
 

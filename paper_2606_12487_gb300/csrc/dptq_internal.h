@@ -164,6 +164,46 @@ inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * kDecodeC
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_kv8_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 
+// ------------------------------------------------------------------ rotary positions, KV4 cache
+struct RotaryArgs {
+  Kv8Args c;               // the batch (no table, no cache)
+  const __half* x;         // rows of `heads` heads, x_stride elements apart
+  __half* out;             // x itself, or rows out_stride apart
+  const uint64_t* turns;   // [rot / 2] fractions of a turn a position, 2^-64 each
+  long long x_stride, out_stride;
+  int heads, head_dim, rot;
+  bool interleaved;
+  float amplitude;
+};
+cudaError_t launch_rotary(const RotaryArgs& a, int num_sms, cudaStream_t s);
+
+struct Kv4Args {
+  Kv8Args c;             // the batch and the pages' sizes (its codes and scales are not used)
+  uint8_t* codes[2];     // K and V: [num_blocks][kv_heads][page][head_dim / 2]
+  uint16_t* scales[2];   // bfloat16 [num_blocks][kv_heads][page]
+};
+struct Kv4RowsArgs {
+  Kv4Args k;
+  __half* rows[2];       // K and V rows of the batch's tokens: read by append, written by read
+  long long stride;
+};
+cudaError_t launch_kv4_append(const Kv4RowsArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_kv4_read(const Kv4RowsArgs& a, int num_sms, cudaStream_t s);
+struct Kv4AttendArgs {
+  Kv4Args k;
+  const __half* q;       // as in Kv8AttendArgs
+  __half* out;
+  long long q_stride, out_stride;
+  int q_heads, group;
+  float scale;
+  int window, sinks;
+  float* ws;
+  uint32_t* counters;
+  long long wait_cycles;
+  int shortfall;
+};
+cudaError_t launch_kv4_decode(const Kv4AttendArgs& a, int num_sms, cudaStream_t s);
+
 // ------------------------------------------------------------------ GEMM
 struct GemmArgs {
   const uint8_t* wt;   // [NTw][KB][4][128][16] packed sign-magnitude weights (chunk-major tiles)

@@ -26,7 +26,9 @@ EXPORTS = ("dptq_pack_weights", "dptq_rotate_quant_act", "dptq_rotate_act", "dpt
            "dptq_last_device_error", "dptq_destroy", "dptq_status_str", "dptq_last_error_message",
            "dptq_pack_weights_rh", "dptq_rotate_quant_act_rh", "dptq_rotate_act_rh", "dptq_kv4_quantize",
            "dptq_sensitivity_policy", "dptq_plan_info", "dptq_launch_plan", "dptq_scratch_buffers",
-           "dptq_add_rmsnorm_quant", "dptq_kv8_append", "dptq_kv8_attention", "dptq_kv8_reserve")
+           "dptq_add_rmsnorm_quant", "dptq_kv8_append", "dptq_kv8_attention", "dptq_kv8_reserve",
+           "dptq_kv4_append", "dptq_kv4_read", "dptq_kv4_attention", "dptq_rotary_frequencies", "dptq_rotary_turns",
+           "dptq_rotary")
 
 
 class _Kv8CacheC(ctypes.Structure):
@@ -37,6 +39,9 @@ class _Kv8CacheC(ctypes.Structure):
 class _Kv8BatchC(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("cu_tokens", "seq_lens", "block_table")] + [
         (n, ctypes.c_int) for n in ("seqs", "table_stride", "tokens", "max_tokens", "max_len")]
+
+
+_Kv4CacheC = _Kv8CacheC      # (the same members; codes and scales of other types)
 
 
 class DptqError(RuntimeError):
@@ -60,7 +65,7 @@ def load(build_if_missing: bool = True):
             if not os.path.exists(path):
                 raise RuntimeError(f"libdptq is not built ({path}); run paper_2606_12487_gb300.build")
             lib = ctypes.CDLL(path)
-            P, I, LL, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float
+            P, I, LL, F, D = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_float, ctypes.c_double
             sig = {
                 "dptq_pack_weights": ([P, I, I, I, I, ctypes.POINTER(P)], I),
                 "dptq_rotate_quant_act": ([P, I, I, I, I, P, P, P], I),
@@ -91,6 +96,12 @@ def load(build_if_missing: bool = True):
                 "dptq_kv8_append": ([P, P, P, P, LL, P], I),
                 "dptq_kv8_attention": ([P, P, P, LL, I, F, I, I, P, LL, P], I),
                 "dptq_kv8_reserve": ([], I),
+                "dptq_kv4_append": ([P, P, P, P, LL, P], I),
+                "dptq_kv4_read": ([P, P, P, P, LL, P], I),
+                "dptq_kv4_attention": ([P, P, P, LL, I, F, I, I, P, LL, P], I),
+                "dptq_rotary_frequencies": ([I, D, I, D, D, D, D, P], I),
+                "dptq_rotary_turns": ([P, I, P], I),
+                "dptq_rotary": ([P, P, LL, I, I, P, I, I, F, P, LL, P], I),
             }
             for name, (args, res) in sig.items():
                 fn = getattr(lib, name)
@@ -359,9 +370,19 @@ class Kv8Batch:
         _check_tensor(block_table, torch.int32, (S, block_table.shape[1]), "block_table")
         self.cu_tokens, self.seq_lens, self.block_table = cu_tokens, seq_lens, block_table
         self.tokens = tokens
+        self.device = seq_lens.get_device()
         self._c = _Kv8BatchC(_ptr(cu_tokens), _ptr(seq_lens), _ptr(block_table), S, block_table.shape[1], tokens,
                              max_tokens, max_len)
         self._ref = ctypes.addressof(self._c)
+
+
+def _check_device(*devices):
+    """A call's tensors lie on the current device, whose stream it is launched on."""
+    import torch
+    now = torch.cuda.current_device()
+    for d in devices:
+        if d != now:
+            raise ValueError(f"tensors must be on the current device ({now}), got one on {d}")
 
 
 def _check_heads(t, tokens, heads, dim, name):
@@ -398,8 +419,136 @@ def dptq_kv8_attention(cache: Kv8Cache, batch: Kv8Batch, q, out, scale: float, w
                                      out.data_ptr(), os_, _stream(stream)))
 
 
+class Kv4Cache:
+    """A paged KV cache of 4-bit codes: codes uint8 [num_blocks, kv_heads, block_tokens, head_dim / 2] (two's
+    complement nibbles, low nibble first) and scales bfloat16 [num_blocks, kv_heads, block_tokens], for K and
+    for V.  Keeps the tensors."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales):
+        import torch
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must have 4 dimensions")
+        n, h, b, d = k_codes.shape
+        _check_tensor(k_codes, torch.uint8, (n, h, b, d), "k_codes")
+        _check_tensor(v_codes, torch.uint8, (n, h, b, d), "v_codes")
+        _check_tensor(k_scales, torch.bfloat16, (n, h, b), "k_scales")
+        _check_tensor(v_scales, torch.bfloat16, (n, h, b), "v_scales")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim = n, h, b, 2 * d
+        self.device = k_codes.get_device()
+        if any(t.get_device() != self.device for t in (v_codes, k_scales, v_scales)):
+            raise ValueError("a cache's tensors must be on one device")
+        self._c = _Kv4CacheC(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), n, h, b, 2 * d)
+        self._ref = ctypes.addressof(self._c)
+
+    @classmethod
+    def empty(cls, num_blocks: int, kv_heads: int, block_tokens: int, head_dim: int, device="cuda"):
+        import torch
+        codes = [torch.zeros((num_blocks, kv_heads, block_tokens, head_dim // 2), dtype=torch.uint8, device=device)
+                 for _ in range(2)]
+        scales = [torch.zeros((num_blocks, kv_heads, block_tokens), dtype=torch.bfloat16, device=device)
+                  for _ in range(2)]
+        return cls(*codes, *scales)
+
+
+def dptq_kv4_append(cache: Kv4Cache, batch: Kv8Batch, k, v, stream=None):
+    """Quantize the new tokens' k and v (as dptq_kv8_append takes them) into the 4-bit cache's pages."""
+    s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
+    if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
+        raise ValueError("k and v must have the same distance between tokens")
+    _check_device(cache.device, batch.device, k.get_device(), v.get_device())
+    _check(load().dptq_kv4_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+
+
+def dptq_kv4_read(cache: Kv4Cache, batch: Kv8Batch, k, v, stream=None):
+    """The cached values of the batch's rows, scale times code, into k and v (float16 [tokens, kv_heads,
+    head_dim], laid out as dptq_kv4_append takes them)."""
+    s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
+    if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
+        raise ValueError("k and v must have the same distance between tokens")
+    _check_device(cache.device, batch.device, k.get_device(), v.get_device())
+    _check(load().dptq_kv4_read(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+
+
+def dptq_kv4_attention(cache: Kv4Cache, batch: Kv8Batch, q, out, scale: float, window: int = 0, sinks: int = 0,
+                       stream=None):
+    """dptq_kv8_attention over the 4-bit cache."""
+    H = q.shape[1]
+    qs = _check_heads(q, batch.tokens, H, cache.head_dim, "q")
+    os_ = _check_heads(out, batch.tokens, H, cache.head_dim, "out")
+    _check_device(cache.device, batch.device, q.get_device(), out.get_device())
+    _check(load().dptq_kv4_attention(cache._ref, batch._ref, q.data_ptr(), qs, H, scale, window, sinks,
+                                     out.data_ptr(), os_, _stream(stream)))
+
+
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "wavelength": 3, "ramp": 4}
+
+
+def dptq_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                            trained_len: float = 0.0, low: float = 1.0, high: float = None):
+    """The angles per position of rot_dim / 2 pairs (float64 numpy array), scaled for contexts beyond
+    trained_len.  low, high: turns of a pair in the trained length up to which it is scaled and from which it
+    is kept (1 and 4 for "wavelength", 1 and 32 for "ramp" if not given)."""
+    import numpy as np
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {tuple(ROTARY_SCALINGS)}")
+    if high is None:
+        high = 32.0 if scaling == "ramp" else 4.0
+    freq = np.empty((max(rot_dim // 2, 1),), dtype=np.float64)
+    _check(load().dptq_rotary_frequencies(rot_dim, base, ROTARY_SCALINGS[scaling], factor, trained_len, low, high,
+                                          freq.ctypes.data))
+    return freq
+
+
+def dptq_rotary_turns(freq):
+    """Angles per position (radians) as 64-bit fractions of a turn (uint64 numpy array)."""
+    import numpy as np
+    freq = np.ascontiguousarray(freq, dtype=np.float64)
+    if freq.ndim != 1:
+        raise ValueError("freq must have one dimension")
+    turns = np.empty(freq.shape, dtype=np.uint64)
+    _check(load().dptq_rotary_turns(freq.ctypes.data, freq.shape[0], turns.ctypes.data))
+    return turns
+
+
+class Rotary:
+    """Rotary positions of the first rot_dim values of a head: the layout of the pairs (neighbours if
+    interleaved, else halves), the amplitude, and the table of frequencies on the GPU, made from the
+    arguments of dptq_rotary_frequencies or given as `frequencies` (radians a position, rot_dim / 2 of them)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                 factor: float = 1.0, trained_len: float = 0.0, low: float = 1.0, high: float = None,
+                 amplitude: float = 1.0, frequencies=None, device="cuda"):
+        import numpy as np
+        import torch
+        if frequencies is None:
+            frequencies = dptq_rotary_frequencies(rot_dim, base, scaling, factor, trained_len, low, high)
+        turns = dptq_rotary_turns(frequencies)
+        if rot_dim % 2 != 0 or turns.shape != (rot_dim // 2,):
+            raise ValueError("rotary positions take rot_dim / 2 frequencies")
+        self.rot_dim, self.interleaved, self.amplitude = rot_dim, bool(interleaved), float(amplitude)
+        self.frequencies = np.asarray(frequencies, dtype=np.float64)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.device = self.turns.get_device()
+
+
+def dptq_rotary(rotary: Rotary, batch: Kv8Batch, x, out=None, stream=None):
+    """Rotary positions of x (float16 [tokens, heads, head_dim], the heads of a token side by side) at the
+    batch's positions, into out (the same shape; x itself if None)."""
+    T, H, D = x.shape
+    xs = _check_heads(x, batch.tokens, H, D, "x")
+    os_ = xs
+    if out is None:
+        out = x
+    else:
+        os_ = _check_heads(out, batch.tokens, H, D, "out")
+    _check_device(rotary.device, batch.device, x.get_device(), out.get_device())
+    _check(load().dptq_rotary(batch._ref, x.data_ptr(), xs, H, D, rotary.turns.data_ptr(), rotary.rot_dim,
+                              rotary.interleaved, rotary.amplitude, out.data_ptr(), os_, _stream(stream)))
+
+
 def dptq_kv8_reserve():
-    """Allocate the scratch of the KV8 calls on the current device."""
+    """Allocate the scratch of the KV8, KV4 and rotary calls on the current device."""
     _check(load().dptq_kv8_reserve())
 
 
