@@ -996,7 +996,8 @@ dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch
   if ((st = fill_attention(a, sc, s, batch, cache->kv_heads, cache->head_dim, q_fp16, q_stride, q_heads, scale, window,
                            sinks, out_fp16, out_stride)) != DPTQ_OK)
     return st;
-  DPTQ_CUDA(launch_kv4_decode(a, sc->num_sms, s), "kv4_attention launch");
+  const bool decode = (long long)a.k.c.max_tokens * a.group <= kDecodeRows;
+  DPTQ_CUDA(decode ? launch_kv4_decode(a, sc->num_sms, s) : launch_kv4_rows(a, sc->num_sms, s), "kv4_attention launch");
   return DPTQ_OK;
 }
 

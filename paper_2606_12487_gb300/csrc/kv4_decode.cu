@@ -1,66 +1,315 @@
-// kv4_decode.cu -- attention over the paged 4-bit cache: a warp a row of a query head, one pass over the keys with
-// the running maximum and sum in fp32.
+// kv4_decode.cu -- attention of a few rows (at most 16 for each sequence and KV head) over the
+// paged 4-bit cache: decode steps and a few speculative tokens.
+//
+// The call is a stream over the visible codes and scales (a byte for two values, read once), so bytes bound it; the
+// codes' way into the tensor cores, about two instructions for three values, is next.  Work is cut into equal
+// shares of steps (kv_decode.cuh); inside a CTA the warps take every fourth step, each with a ring of steps of its
+// own in shared memory, filled by asynchronous 16-byte copies (no barrier between warps).
+//
+// A warp multiplies with 16 x 8 x 16 register MMAs, codes first (keys x rows of q, then dims x rows):
+//   * logits: the A fragment of key g takes any order of the dims as long as q has the same, so a lane takes
+//     D / 4 consecutive dims of its keys, and the pairs (0, 4), (1, 5), .. that a word widens to;
+//   * values: the A fragment of dim g takes any order of the dims across its tiles, so a lane takes D / 8
+//     consecutive dims of four keys; the 16-bit halves of two keys' words make pairs (key, key).
+// Each 32-byte part of a 128-byte line stands at its place xor the line's number mod 4, so that neither
+// read meets a bank twice.
+//
+// Softmax in base 2 on x_j = log2(e) scale sk (q . ck_j) + log2(sv): codes are the exact operands, scales
+// stay in fp32, and the weights that go into the second product are p_j sv_j relative to 2^-15 of the largest of
+// them: binary16 holds 29 binades of those without loss.  The denominator takes each back by 1 / sv.
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
 
 #include "kv4_device.cuh"
+#include "kv_decode.cuh"
 
 namespace dptq {
 
-template <int D>
-__global__ void __launch_bounds__(256) kv4_rows_kernel(const Kv4AttendArgs A) {
-  constexpr int E = D / 32;
+// A warp's ring: steps of 16 NG keys, K codes, then V codes, and what goes with a step.
+template <int D, int NG>
+struct alignas(128) Ring4 {
+  static constexpr int kKeys = 16 * NG, kHalf = kKeys * D / 2;   // bytes of K (and of V)
+  static constexpr int kStages = 8192 / kHalf;                   // 16 KB a warp
+  uint8_t kv[kStages][2 * kHalf];
+  uint16_t scale[kStages][2][kKeys];
+  uint32_t held[kStages];                                        // bit h: the page of keys 16 h .. is there
+};
+// Where byte `at` of a half of a step stands.
+__device__ __forceinline__ uint32_t swz32(uint32_t at) { return at ^ (((at >> 7) & 3u) << 5); }
+__device__ __forceinline__ uint32_t bits(const __half2& h) { return *reinterpret_cast<const uint32_t*>(&h); }
+
+constexpr float kDecUnit = 15.f;   // weights are relative to 2^-15 of the largest
+
+template <int D, int RT, int NG>   // RT: tiles of 8 rows (1 or 2)
+__global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeCtas16)
+kv4_decode_kernel(const Kv4AttendArgs A) {
+  using Ring = Ring4<D, NG>;
+  constexpr int KW = D / 32, VW = D / 64, VB = D / 8;   // words of a K and V row, and dims of a V row, for a lane
+  constexpr int R = 8 * RT, NS = Ring::kStages, H = Ring::kHalf, kKeys = Ring::kKeys;
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ JoinShared<R> S;
   const Kv8Args& c = A.k.c;
-  const int lane = threadIdx.x & 31, head = blockIdx.z, row = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int P = 1 << c.log2_page;
+  Ring& ring = reinterpret_cast<Ring*>(sm)[warp];   // (becomes the warp's weighted values [R][D] at a share's end)
+
   pdl_launch_dependents();
   pdl_wait();
-  Seq q;
-  if (!load_seq(c, blockIdx.y, q, threadIdx.x == 0 && blockIdx.x == 0 && head == 0) || row >= q.n) return;
-  const int pos = q.start + row, P1 = (1 << c.log2_page) - 1, kvh = head / A.group;
-  const __half* src = A.q + (size_t)(q.tok0 + row) * A.q_stride + (size_t)head * D + E * lane;
-  float x[E], o[E], m = -INFINITY, l = 0.f;
+
+  decode_shares<D, R, kKeys>(c, A, S, sm, sizeof(Ring), [&](const Seq& q, int s, const Steps& st, int head, int i0, int i1) {
+    const int rows = q.n * A.group;
+    // ---- this share's rows of q, in the order of the dims that a widened word has
+    uint32_t qf[RT][D / 16][2];
+    int pos[RT][2];   // positions of the two rows whose logits this lane holds
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = __half2float(ld_plain(src + e)), o[e] = 0.f;
-  for (int j = 0; j <= pos; ++j) {
-    if (!kv8_sees(pos, j, A.window, A.sinks)) {
-      j = max(j, pos - A.window);
-      continue;
-    }
-    const int b = load_page(c, blockIdx.y, j >> c.log2_page);
-    if (b < 0) continue;
-    const size_t at = (((size_t)b * c.kv_heads + kvh) << c.log2_page) + (j & P1);
-    float k[E], v[E];
-    const float sk = bf16_float(ld_plain(A.k.scales[0] + at)), sv = bf16_float(ld_plain(A.k.scales[1] + at));
+    for (int r = 0; r < RT; ++r) {
+      // (lanes without a row read the first one: a load in a branch would wait for its own data)
+      const int row = g + 8 * r < rows ? g + 8 * r : 0, tok = row / A.group, hh = row - tok * A.group;
+      const __half* src = A.q + (size_t)(q.tok0 + tok) * A.q_stride + (size_t)(head * A.group + hh) * D + D / 4 * t;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const int w = ld_plain(A.k.codes[kv] + at * (D / 2) + (E * lane + e) / 2);
-        (kv ? v : k)[e] = (float)((w << 28) >> 28);
-        (kv ? v : k)[e + 1] = (float)((w << 24) >> 28);
+      for (int w = 0; w < KW; ++w) {
+        const uint4 v = ld_plain(reinterpret_cast<const uint4*>(src) + w);
+        qf[r][2 * w][0] = __byte_perm(v.x, v.z, 0x5410);
+        qf[r][2 * w][1] = __byte_perm(v.x, v.z, 0x7632);
+        qf[r][2 * w + 1][0] = __byte_perm(v.y, v.w, 0x5410);
+        qf[r][2 * w + 1][1] = __byte_perm(v.y, v.w, 0x7632);
       }
-    float t = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) t = fmaf(x[e], k[e], t);
+      for (int e = 0; e < 2; ++e) {
+        const int mine = 8 * r + 2 * t + e;
+        pos[r][e] = mine < rows ? q.start + mine / A.group : -1;
+      }
+    }
+    // weighted values of two rows, dims VB g + 2 j and the next
+    float o[RT][VB / 2][4], m[RT][2], l[RT][2];
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) t += __shfl_xor_sync(0xffffffffu, t, w);
-    t *= isfinite(sk) && isfinite(sv) ? sk * A.scale : NAN;
-    const float mn = t > m ? t : m, f = m == -INFINITY ? 0.f : __expf(m - mn), p = t == -INFINITY ? 0.f : __expf(t - mn);
-    m = mn;
-    l = fmaf(l, f, p);
+    for (int r = 0; r < RT; ++r) {
+      m[r][0] = m[r][1] = -INFINITY;
+      l[r][0] = l[r][1] = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], f, p * (isfinite(sv) ? sv * v[e] : 0.f));
-  }
-  __half* dst = A.out + (size_t)(q.tok0 + row) * A.out_stride + (size_t)head * D + E * lane;
+      for (int j = 0; j < VB / 2; ++j)
 #pragma unroll
-  for (int e = 0; e < E; ++e) dst[e] = __float2half_rn(l == 0.f ? 0.f : o[e] / l);
+        for (int e = 0; e < 4; ++e) o[r][j][e] = 0.f;
+    }
+
+    // ---- the steps of this warp
+    auto key_of = [&](int i) { return i < st.sink ? i * kKeys : st.from + (i - st.sink) * kKeys; };
+    // Lane h: the page of the step's keys 16 h .., or -1 (pages that no row sees are not looked up)
+    auto page_of = [&](int i) {
+      if (i >= i1 || lane >= NG) return -1;
+      const int k = key_of(i) + 16 * lane;
+      const bool seen = k < q.len && (A.window == 0 || k + 15 > (q.start > 0 ? q.start : 0) - A.window || k < A.sinks);
+      return seen ? load_page(c, s, k >> c.log2_page) : -1;
+    };
+    // copies step i into its stage; always one group, so that the waits can count
+    auto issue = [&](int i, int stage, int page) {
+      if (i < i1) {
+        const int in = key_of(i) & (P - 1);
+        const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
+        auto row_of = [&](int h) {   // of the cache, of the step's key 16 h
+          const int b = max(__shfl_sync(0xffffffffu, page, h), 0);
+          return (((size_t)b * c.kv_heads + head) << c.log2_page) + ((in + 16 * h) & (P - 1));
+        };
+#pragma unroll
+        for (int h = 0; h < NG; ++h) {
+          const size_t at = row_of(h) * (D / 2) + 16 * lane;
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int u = 0; u < D / 64; ++u)
+              copy16(smem_u32(ring.kv[stage]) + kv * H + swz32(8 * D * h + 512 * u + 16 * lane),
+                     A.k.codes[kv] + at + 512 * u, held >> h & 1u);
+        }
+        const int h = (lane >> 1) % NG, kv = lane / (2 * NG), part = 8 * (lane & 1);
+        const size_t row = row_of(h) + part;
+        if (lane < 4 * NG)
+          copy16(smem_u32(&ring.scale[stage][kv][16 * h + part]), (kv ? A.k.scales[1] : A.k.scales[0]) + row, held >> h & 1u);
+        if (lane == 0) ring.held[stage] = held;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    int i = i0 + warp, stage = 0;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) issue(i + k * kDecWarps, k, page_of(i + k * kDecWarps));
+    for (; i < i1; i += kDecWarps) {
+      const int page = page_of(i + NS * kDecWarps);   // (used after this step)
+      asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
+      __syncwarp();
+      const uint8_t* ck = ring.kv[stage];
+      const uint8_t* cv = ck + H;
+      const uint32_t held = ring.held[stage];
+      const int key = key_of(i);
+      // logits of 16 keys and 8 rows: keys g, g + 8, rows 2 t, 2 t + 1
+      float x[NG][RT][4], inv[NG][2];
+#pragma unroll
+      for (int h = 0; h < NG; ++h) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[h][r][e] = 0.f;
+        uint32_t w0[KW], w1[KW];
+        const uint8_t* p0 = ck + swz32((16 * h + g) * (D / 2) + D / 8 * t);
+        const uint8_t* p1 = ck + swz32((16 * h + 8 + g) * (D / 2) + D / 8 * t);
+        if constexpr (D == 128) {
+          const uint4 a = *reinterpret_cast<const uint4*>(p0), b = *reinterpret_cast<const uint4*>(p1);
+          w0[0] = a.x, w0[1] = a.y, w0[2] = a.z, w0[3] = a.w;
+          w1[0] = b.x, w1[1] = b.y, w1[2] = b.z, w1[3] = b.w;
+        } else {
+          const uint2 a = *reinterpret_cast<const uint2*>(p0), b = *reinterpret_cast<const uint2*>(p1);
+          w0[0] = a.x, w0[1] = a.y;
+          w1[0] = b.x, w1[1] = b.y;
+        }
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          __half2 a[4], b[4];
+          widen8(w0[w], a);
+          widen8(w1[w], b);
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              mma_16816(x[h][r], bits(a[2 * k]), bits(b[2 * k]), bits(a[2 * k + 1]), bits(b[2 * k + 1]),
+                        qf[r][2 * w + k][0], qf[r][2 * w + k][1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {   // a key's factor and addend
+          const float sk = bf16_float(ring.scale[stage][0][16 * h + g + 8 * e]);
+          const float sv = bf16_float(ring.scale[stage][1][16 * h + g + 8 * e]);
+          const float v = fmaxf(sv, 0x1p-40f);   // (zeros, which add nothing)
+          // (what is not seen is masked below: a scale that is no number stays with the rows that see it)
+          const float fa = sk * (A.scale * 1.4426950408889634f), fb = isfinite(sk) && isfinite(sv) ? __log2f(v) : NAN;
+          inv[h][e] = __frcp_rn(v);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            x[h][r][2 * e] = fmaf(x[h][r][2 * e], fa, fb);
+            x[h][r][2 * e + 1] = fmaf(x[h][r][2 * e + 1], fa, fb);
+          }
+        }
+      }
+      // every row sees every key of the step
+      const bool all = held == (1u << NG) - 1 && key + kKeys - 1 <= q.start &&
+                       (A.window == 0 || key > q.len - 1 - A.window || key + kKeys <= A.sinks);
+      if (!all) {
+#pragma unroll
+        for (int h = 0; h < NG; ++h)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!((held >> h & 1u) && kv8_sees(pos[r][e & 1], key + 16 * h + g + 8 * (e >> 1), A.window, A.sinks)))
+                x[h][r][e] = -INFINITY;
+      }
+      float top[RT][2];
+      bool grown = false;
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float v = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < NG; ++h) v = fmaxf(v, fmaxf(x[h][r][e], x[h][r][e + 2]));
+          grown |= v > m[r][e];
+          top[r][e] = fmaxf(v, m[r][e]);
+        }
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) top[r][e] = fmaxf(top[r][e], __shfl_xor_sync(0xffffffffu, top[r][e], w));
+            const float f = top[r][e] == m[r][e] ? 1.f : exp2_fast(m[r][e] - top[r][e]);
+            m[r][e] = top[r][e];
+            l[r][e] *= f;
+#pragma unroll
+            for (int j = 0; j < VB / 2; ++j) o[r][j][e] *= f, o[r][j][e + 2] *= f;
+          }
+      }
+      uint32_t pf[NG][RT][2];   // B fragments of the weights, per 16 keys
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float m0 = m[r][0] == -INFINITY ? 0.f : m[r][0] - kDecUnit, m1 = m[r][1] == -INFINITY ? 0.f : m[r][1] - kDecUnit;
+#pragma unroll
+        for (int h = 0; h < NG; ++h) {
+          const float p0 = exp2_fast(x[h][r][0] - m0), p1 = exp2_fast(x[h][r][1] - m1);
+          const float p2 = exp2_fast(x[h][r][2] - m0), p3 = exp2_fast(x[h][r][3] - m1);
+          l[r][0] = fmaf(p0, inv[h][0], fmaf(p2, inv[h][1], l[r][0]));
+          l[r][1] = fmaf(p1, inv[h][0], fmaf(p3, inv[h][1], l[r][1]));
+          pf[h][r][0] = transpose8x8(pack_half2(p0, p1));
+          pf[h][r][1] = transpose8x8(pack_half2(p2, p3));
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < NG; ++h) {
+        uint32_t vw[4][VW];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {   // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+          const uint8_t* p = cv + swz32((16 * h + 2 * t + (u >> 1) * 8 + (u & 1)) * (D / 2) + D / 16 * g);
+          if constexpr (D == 128) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            vw[u][0] = v.x, vw[u][1] = v.y;
+          } else {
+            vw[u][0] = *reinterpret_cast<const uint32_t*>(p);
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {   // dims 8 w + 4 k .. of the lane's
+            __half2 a[4], b[4];
+            widen8(__byte_perm(vw[0][w], vw[1][w], k ? 0x7632 : 0x5410), a);
+            widen8(__byte_perm(vw[2][w], vw[3][w], k ? 0x7632 : 0x5410), b);
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                mma_16816(o[r][4 * w + 2 * k + j], bits(a[2 * j]), bits(a[2 * j + 1]), bits(b[2 * j]), bits(b[2 * j + 1]),
+                          pf[h][r][0], pf[h][r][1]);
+          }
+      }
+      __syncwarp();
+      issue(i + NS * kDecWarps, stage, page);
+      stage = stage + 1 == NS ? 0 : stage + 1;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int row = 8 * r + 2 * t + e;
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[r][e] += __shfl_xor_sync(0xffffffffu, l[r][e], w);
+        float* dst = reinterpret_cast<float*>(&ring) + row * D + VB * g;
+#pragma unroll
+        for (int j = 0; j < VB / 2; ++j) *reinterpret_cast<float2*>(dst + 2 * j) = make_float2(o[r][j][e], o[r][j][e + 2]);
+        if (g == 0) {
+          S.m[warp][row] = m[r][e];
+          S.l[warp][row] = l[r][e];
+        }
+      }
+  });
+}
+
+template <int D, int RT>
+static cudaError_t launch_decode4(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int NG = 4;
+  const auto fn = kv4_decode_kernel<D, RT, NG>;
+  const size_t smem = sizeof(Ring4<D, NG>) * kDecWarps;
+  const cudaError_t e = ensure_max_dyn_smem(fn);
+  if (e != cudaSuccess) return e;
+  static_assert(kDecodeCtas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)
+  if (num_sms > 256) return cudaErrorInvalidValue;
+  return launch_after(fn, num_sms * (RT == 1 ? kDecodeCtas8 : kDecodeCtas16), kDecThreads, smem, s, 1, a);
 }
 
 cudaError_t launch_kv4_decode(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
-  const dim3 grid(ceil_div(a.k.c.max_tokens, 8), a.k.c.seqs, a.q_heads);
-  return a.k.c.head_dim == 64 ? launch_after(kv4_rows_kernel<64>, grid, 256, 0, s, 1, a)
-                              : launch_after(kv4_rows_kernel<128>, grid, 256, 0, s, 1, a);
+  const bool one = a.k.c.max_tokens * a.group <= 8;
+  if (a.k.c.head_dim == 64) return one ? launch_decode4<64, 1>(a, num_sms, s) : launch_decode4<64, 2>(a, num_sms, s);
+  return one ? launch_decode4<128, 1>(a, num_sms, s) : launch_decode4<128, 2>(a, num_sms, s);
 }
 
 }  // namespace dptq
