@@ -271,7 +271,8 @@ dptq_status dptq_kv8_reserve(void);
  * [num_blocks][kv_heads][block_tokens].  Codes and scales 16-byte aligned.  A cached value is
  * binary16(scale * code), which is exact for scales of 2^-17 and more (8 + 3 significant bits): the tensor
  * cores, the read-back and the definition below all see the same values.  head_dim 64 or 128;
- * block_tokens 16, 32, 64 or 128.  All device memory of the caller; the struct is read during the call only. */
+ * block_tokens 16, 32, 64 or 128; num_blocks * kv_heads * block_tokens below 2^32 (UNSUPPORTED otherwise).
+ * All device memory of the caller; the struct is read during the call only. */
 typedef struct dptq_kv4_cache {
   uint8_t* k_codes;
   uint8_t* v_codes;

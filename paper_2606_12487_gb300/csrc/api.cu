@@ -856,6 +856,9 @@ dptq_status check_kv8(const dptq_kv8_cache* c, const dptq_kv8_batch* b, cudaStre
 }
 dptq_status check_kv4(const dptq_kv4_cache* c, const dptq_kv8_batch* b, cudaStream_t s, Kv4Args* a, bool* none,
                       Scratch** sc) {
+  if (c && c->num_blocks > 0 && c->kv_heads > 0 && c->block_tokens > 0 &&
+      (double)c->num_blocks * c->kv_heads * c->block_tokens > 4294967295.0)
+    return fail(DPTQ_ERR_UNSUPPORTED, "a cache of 2^32 tokens and heads or more");
   // (16 scales of a page's tokens are read at a time)
   const dptq_status st = check_paged(c, b, 16, s, &a->c, none, sc);
   if (st != DPTQ_OK || *none) return st;

@@ -154,13 +154,13 @@ struct Kv8AttendArgs {
 constexpr int kDecodeRows = 16;
 // Decode grids: CTAs an SM for up to 8 and up to 16 rows; each CTA leaves partial results of two
 // (sequence, head)s at most: weighted values, maximum and sum of each row.
-constexpr int kDecodeCtas8 = 3, kDecodeCtas16 = 2;
+constexpr int kDecodeCtas8 = 3, kDecodeCtas16 = 2, kDecode4Ctas8 = 3;   // (kDecode4Ctas8: of the 4-bit cache)
 // A prompt's grid that is split along the keys has at most a CTA an SM, of 256 rows.
 inline size_t kv8_ws_bytes(int num_sms) {
   const int r8 = 2 * kDecodeCtas8 * 8, r16 = 2 * kDecodeCtas16 * 16, r = r8 > r16 ? r8 : r16;
   return (size_t)num_sms * (r > 256 ? r : 256) * (128 + 2) * sizeof(float);
 }
-inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * kDecodeCtas8 * 3; }
+inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * 4 * 3; }
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_kv8_prefill(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);
 

@@ -30,19 +30,79 @@ namespace dptq {
 template <int D, int NG>
 struct alignas(128) Ring4 {
   static constexpr int kKeys = 16 * NG, kHalf = kKeys * D / 2;   // bytes of K (and of V)
-  static constexpr int kStages = 8192 / kHalf;                   // 16 KB a warp
+  static constexpr int kStages = (NG == 2 ? 6144 : 8192) / kHalf;
   uint8_t kv[kStages][2 * kHalf];
   uint16_t scale[kStages][2][kKeys];
-  uint32_t held[kStages];                                        // bit h: the page of keys 16 h .. is there
+  float4 factor[kKeys];      // of a step's keys: x = a S + b; 1 / sv
+  uint32_t held[kStages];    // bit h: the page of keys 16 h .. is there
 };
-// Where byte `at` of a half of a step stands.
-__device__ __forceinline__ uint32_t swz32(uint32_t at) { return at ^ (((at >> 7) & 3u) << 5); }
+// (a page that is not there reads page 0: its keys are masked)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// Where byte `at` of a half of a step stands: 32-byte parts of the lines of 8 rows.
+template <int D>
+__device__ __forceinline__ uint32_t swz32(uint32_t at) {
+  return at ^ (((at >> 7) & (D / 32 - 1u)) << 5);
+}
 __device__ __forceinline__ uint32_t bits(const __half2& h) { return *reinterpret_cast<const uint32_t*>(&h); }
 
+__device__ __forceinline__ float log2_fast(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Constants in registers: (w & mask) ^ flip is then one instruction.
+struct Nibbles {
+  uint32_t lo, hi, tiny_lo, tiny_hi, wide_lo, wide_hi;
+  __device__ __forceinline__ Nibbles() {
+    asm("mov.b32 %0, 0x000F000F;" : "=r"(lo));
+    asm("mov.b32 %0, 0x00F000F0;" : "=r"(hi));
+    asm("mov.b32 %0, 0x00080008;" : "=r"(tiny_lo));
+    asm("mov.b32 %0, 0x00800080;" : "=r"(tiny_hi));
+    asm("mov.b32 %0, 0x64086408;" : "=r"(wide_lo));
+    asm("mov.b32 %0, 0x64806480;" : "=r"(wide_hi));
+  }
+  static __device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+  }
+  // Nibbles 0 and 4 (HI: 1 and 5) of a word, plus 8, as binary16 numbers below its normal range: (code + 8) 2^-24 (HI:
+  // 2^-20).
+  template <bool HI>
+  __device__ __forceinline__ uint32_t tiny(uint32_t w) const {
+    return HI ? and_xor(w, hi, tiny_hi) : and_xor(w, lo, tiny_lo);
+  }
+  // Eight codes to four pairs of binary16, in the order 0 4, 1 5, 2 6, 3 7: under the exponent of 1024 a nibble reads
+  // 1032 + code, four bits higher 1024 + 16 (code + 8); one subtraction or fma, exact, takes the offset off.
+  __device__ __forceinline__ void widen(uint32_t w, __half2 (&r)[4]) const {
+    const __half2 off = __half2half2(__ushort_as_half(0x6408));                                                         // 1032
+    const __half2 sixteenth = __half2half2(__ushort_as_half(0x2C00)), off16 = __half2half2(__ushort_as_half(0xD480));   // 1 / 16, -72
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t v = k ? w >> 8 : w, a = and_xor(v, lo, wide_lo), b = and_xor(v, hi, wide_hi);
+      r[2 * k] = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
+      r[2 * k + 1] = __hfma2(*reinterpret_cast<const __half2*>(&b), sixteenth, off16);
+    }
+  }
+};
+
+constexpr int kNG = 4;
 constexpr float kDecUnit = 15.f;   // weights are relative to 2^-15 of the largest
 
 template <int D, int RT, int NG>   // RT: tiles of 8 rows (1 or 2)
-__global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecodeCtas8 : kDecodeCtas16)
+__global__ void __launch_bounds__(kDecThreads, RT == 1 ? kDecode4Ctas8 : kDecodeCtas16)
 kv4_decode_kernel(const Kv4AttendArgs A) {
   using Ring = Ring4<D, NG>;
   constexpr int KW = D / 32, VW = D / 64, VB = D / 8;   // words of a K and V row, and dims of a V row, for a lane
@@ -54,6 +114,16 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
   const int P = 1 << c.log2_page;
   Ring& ring = reinterpret_cast<Ring*>(sm)[warp];   // (becomes the warp's weighted values [R][D] at a share's end)
 
+  // Where a lane's copies go, and its reads of K and V come from, within a step (8 and 16 keys on, the swizzle is the same).
+  const uint32_t to_lane = smem_u32(ring.kv[0]) + swz32<D>(16 * lane), k_lane = swz32<D>(g * (D / 2) + D / 8 * t);
+  const uint32_t v_lane[2] = {swz32<D>(2 * t * (D / 2) + D / 16 * g), swz32<D>((2 * t + 1) * (D / 2) + D / 16 * g)};
+  // (scales: lanes 2 h and 2 h + 1 copy K's of the step's keys 16 h .., the next 2 NG lanes V's)
+  const uint32_t to_scale = smem_u32(ring.scale[0][lane / (2 * NG) & 1]) + 16 * (lane % (2 * NG));
+  const uint8_t *k_from = A.k.codes[0] + 16 * lane, *v_from = A.k.codes[1] + 16 * lane;
+  const uint8_t* s_from = reinterpret_cast<const uint8_t*>(lane / (2 * NG) ? A.k.scales[1] : A.k.scales[0]) + 16 * (lane & 1);
+  const Nibbles nib;
+  const float unit = A.scale * (1.4426950408889634f * 0x1p24f);
+
   pdl_launch_dependents();
   pdl_wait();
 
@@ -61,7 +131,8 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
     const int rows = q.n * A.group;
     // ---- this share's rows of q, in the order of the dims that a widened word has
     uint32_t qf[RT][D / 16][2];
-    int pos[RT][2];   // positions of the two rows whose logits this lane holds
+    float off[RT][2];   // -8 2^-24 times the sum of q, of the two rows whose logits this lane holds
+    int pos[RT][2];     // their positions
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       // (lanes without a row read the first one: a load in a branch would wait for its own data)
@@ -70,15 +141,27 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
         const uint4 v = ld_plain(reinterpret_cast<const uint4*>(src) + w);
+        // nibbles (0, 4), (2, 6) and (1, 5), (3, 7) together
         qf[r][2 * w][0] = __byte_perm(v.x, v.z, 0x5410);
-        qf[r][2 * w][1] = __byte_perm(v.x, v.z, 0x7632);
-        qf[r][2 * w + 1][0] = __byte_perm(v.y, v.w, 0x5410);
+        qf[r][2 * w][1] = __byte_perm(v.y, v.w, 0x5410);
+        qf[r][2 * w + 1][0] = __byte_perm(v.x, v.z, 0x7632);
         qf[r][2 * w + 1][1] = __byte_perm(v.y, v.w, 0x7632);
       }
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&qf[r][k][e]));
+          sum += f.x + f.y;
+        }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);   // (of row g)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int mine = 8 * r + 2 * t + e;
         pos[r][e] = mine < rows ? q.start + mine / A.group : -1;
+        off[r][e] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t + e));
       }
     }
     // weighted values of two rows, dims VB g + 2 j and the next
@@ -107,24 +190,23 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
       if (i < i1) {
         const int in = key_of(i) & (P - 1);
         const uint32_t held = __ballot_sync(0xffffffffu, page >= 0);
-        auto row_of = [&](int h) {   // of the cache, of the step's key 16 h
-          const int b = max(__shfl_sync(0xffffffffu, page, h), 0);
-          return (((size_t)b * c.kv_heads + head) << c.log2_page) + ((in + 16 * h) & (P - 1));
+        const int from = max(page, 0);
+        auto row_of = [&](int h) {   // of the cache, of the step's key 16 h (fewer than 2^32, checked on the host)
+          return ((unsigned)__shfl_sync(0xffffffffu, from, h) * c.kv_heads + head) * P + ((in + 16 * h) & (P - 1));
         };
+        const uint32_t dst = to_lane + stage * (2 * H);
 #pragma unroll
         for (int h = 0; h < NG; ++h) {
-          const size_t at = row_of(h) * (D / 2) + 16 * lane;
+          const unsigned row = row_of(h);
+          const uint8_t *ks = k_from + (unsigned long long)row * (D / 2), *vs = v_from + (unsigned long long)row * (D / 2);
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-            for (int u = 0; u < D / 64; ++u)
-              copy16(smem_u32(ring.kv[stage]) + kv * H + swz32(8 * D * h + 512 * u + 16 * lane),
-                     A.k.codes[kv] + at + 512 * u, held >> h & 1u);
+          for (int u = 0; u < D / 64; ++u) {
+            copy16(dst + 8 * D * h + 512 * u, ks + 512 * u);
+            copy16(dst + H + 8 * D * h + 512 * u, vs + 512 * u);
+          }
         }
-        const int h = (lane >> 1) % NG, kv = lane / (2 * NG), part = 8 * (lane & 1);
-        const size_t row = row_of(h) + part;
-        if (lane < 4 * NG)
-          copy16(smem_u32(&ring.scale[stage][kv][16 * h + part]), (kv ? A.k.scales[1] : A.k.scales[0]) + row, held >> h & 1u);
+        const unsigned row = row_of((lane >> 1) % NG);
+        if (lane < 4 * NG) copy16(to_scale + stage * (4 * kKeys), s_from + (unsigned long long)row * 2);
         if (lane == 0) ring.held[stage] = held;
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -141,17 +223,26 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
       const uint8_t* cv = ck + H;
       const uint32_t held = ring.held[stage];
       const int key = key_of(i);
+      // a key's factor and addend, made by a lane for all
+#pragma unroll
+      for (int k = lane; k < kKeys; k += 32) {
+        const float sk = bf16_float(ring.scale[stage][0][k]), sv = bf16_float(ring.scale[stage][1][k]);
+        const float v = fmaxf(sv, 0x1p-40f);   // (zeros, which add nothing)
+        // (NaN for a scale that is no number; what is not seen is masked below, so it stays with the rows that see it)
+        ring.factor[k] = make_float4(sk * unit, fmaf(sk + sv, 0.f, log2_fast(v)), rcp_fast(v), 0.f);
+      }
       // logits of 16 keys and 8 rows: keys g, g + 8, rows 2 t, 2 t + 1
-      float x[NG][RT][4], inv[NG][2];
+      float x[NG][RT][4];
 #pragma unroll
       for (int h = 0; h < NG; ++h) {
+        float y[RT][4];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[h][r][e] = 0.f;
+          for (int e = 0; e < 4; ++e) x[h][r][e] = off[r][e & 1], y[r][e] = 0.f;
         uint32_t w0[KW], w1[KW];
-        const uint8_t* p0 = ck + swz32((16 * h + g) * (D / 2) + D / 8 * t);
-        const uint8_t* p1 = ck + swz32((16 * h + 8 + g) * (D / 2) + D / 8 * t);
+        const uint8_t* p0 = ck + k_lane + 8 * D * h;
+        const uint8_t* p1 = p0 + 4 * D;
         if constexpr (D == 128) {
           const uint4 a = *reinterpret_cast<const uint4*>(p0), b = *reinterpret_cast<const uint4*>(p1);
           w0[0] = a.x, w0[1] = a.y, w0[2] = a.z, w0[3] = a.w;
@@ -163,31 +254,32 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         }
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
-          __half2 a[4], b[4];
-          widen8(w0[w], a);
-          widen8(w1[w], b);
-#pragma unroll
-          for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-              mma_16816(x[h][r], bits(a[2 * k]), bits(b[2 * k]), bits(a[2 * k + 1]), bits(b[2 * k + 1]),
-                        qf[r][2 * w + k][0], qf[r][2 * w + k][1]);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {   // a key's factor and addend
-          const float sk = bf16_float(ring.scale[stage][0][16 * h + g + 8 * e]);
-          const float sv = bf16_float(ring.scale[stage][1][16 * h + g + 8 * e]);
-          const float v = fmaxf(sv, 0x1p-40f);   // (zeros, which add nothing)
-          // (what is not seen is masked below: a scale that is no number stays with the rows that see it)
-          const float fa = sk * (A.scale * 1.4426950408889634f), fb = isfinite(sk) && isfinite(sv) ? __log2f(v) : NAN;
-          inv[h][e] = __frcp_rn(v);
+          const uint32_t s0 = w0[w] >> 8, s1 = w1[w] >> 8;
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
-            x[h][r][2 * e] = fmaf(x[h][r][2 * e], fa, fb);
-            x[h][r][2 * e + 1] = fmaf(x[h][r][2 * e + 1], fa, fb);
+            mma_16816(x[h][r], nib.tiny<false>(w0[w]), nib.tiny<false>(w1[w]), nib.tiny<false>(s0), nib.tiny<false>(s1), qf[r][2 * w][0],
+                      qf[r][2 * w][1]);
+            mma_16816(y[r], nib.tiny<true>(w0[w]), nib.tiny<true>(w1[w]), nib.tiny<true>(s0), nib.tiny<true>(s1), qf[r][2 * w + 1][0],
+                      qf[r][2 * w + 1][1]);
           }
         }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[h][r][e] = fmaf(y[r][e], 0x1p-4f, x[h][r][e]);
       }
+      __syncwarp();
+#pragma unroll
+      for (int h = 0; h < NG; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float2 f = *reinterpret_cast<const float2*>(&ring.factor[16 * h + g + 8 * e]);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            x[h][r][2 * e] = fmaf(x[h][r][2 * e], f.x, f.y);
+            x[h][r][2 * e + 1] = fmaf(x[h][r][2 * e + 1], f.x, f.y);
+          }
+        }
       // every row sees every key of the step
       const bool all = held == (1u << NG) - 1 && key + kKeys - 1 <= q.start &&
                        (A.window == 0 || key > q.len - 1 - A.window || key + kKeys <= A.sinks);
@@ -209,7 +301,7 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         for (int e = 0; e < 2; ++e) {
           float v = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < NG; ++h) v = fmaxf(v, fmaxf(x[h][r][e], x[h][r][e + 2]));
+          for (int h = 0; h < NG; ++h) v = max3(v, x[h][r][e], x[h][r][e + 2]);
           grown |= v > m[r][e];
           top[r][e] = fmaxf(v, m[r][e]);
         }
@@ -235,8 +327,9 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         for (int h = 0; h < NG; ++h) {
           const float p0 = exp2_fast(x[h][r][0] - m0), p1 = exp2_fast(x[h][r][1] - m1);
           const float p2 = exp2_fast(x[h][r][2] - m0), p3 = exp2_fast(x[h][r][3] - m1);
-          l[r][0] = fmaf(p0, inv[h][0], fmaf(p2, inv[h][1], l[r][0]));
-          l[r][1] = fmaf(p1, inv[h][0], fmaf(p3, inv[h][1], l[r][1]));
+          const float i0 = ring.factor[16 * h + g].z, i1 = ring.factor[16 * h + g + 8].z;
+          l[r][0] = fmaf(p0, i0, fmaf(p2, i1, l[r][0]));
+          l[r][1] = fmaf(p1, i0, fmaf(p3, i1, l[r][1]));
           pf[h][r][0] = transpose8x8(pack_half2(p0, p1));
           pf[h][r][1] = transpose8x8(pack_half2(p2, p3));
         }
@@ -246,7 +339,7 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         uint32_t vw[4][VW];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {   // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-          const uint8_t* p = cv + swz32((16 * h + 2 * t + (u >> 1) * 8 + (u & 1)) * (D / 2) + D / 16 * g);
+          const uint8_t* p = cv + v_lane[u & 1] + 8 * D * h + 4 * D * (u >> 1);
           if constexpr (D == 128) {
             const uint2 v = *reinterpret_cast<const uint2*>(p);
             vw[u][0] = v.x, vw[u][1] = v.y;
@@ -259,8 +352,8 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {   // dims 8 w + 4 k .. of the lane's
             __half2 a[4], b[4];
-            widen8(__byte_perm(vw[0][w], vw[1][w], k ? 0x7632 : 0x5410), a);
-            widen8(__byte_perm(vw[2][w], vw[3][w], k ? 0x7632 : 0x5410), b);
+            nib.widen(__byte_perm(vw[0][w], vw[1][w], k ? 0x7632 : 0x5410), a);
+            nib.widen(__byte_perm(vw[2][w], vw[3][w], k ? 0x7632 : 0x5410), b);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -296,14 +389,14 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
 
 template <int D, int RT>
 static cudaError_t launch_decode4(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int NG = 4;
+  constexpr int NG = RT == 1 ? kNG : 2;
   const auto fn = kv4_decode_kernel<D, RT, NG>;
   const size_t smem = sizeof(Ring4<D, NG>) * kDecWarps;
   const cudaError_t e = ensure_max_dyn_smem(fn);
   if (e != cudaSuccess) return e;
-  static_assert(kDecodeCtas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)
+  static_assert(kDecode4Ctas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)
   if (num_sms > 256) return cudaErrorInvalidValue;
-  return launch_after(fn, num_sms * (RT == 1 ? kDecodeCtas8 : kDecodeCtas16), kDecThreads, smem, s, 1, a);
+  return launch_after(fn, num_sms * (RT == 1 ? kDecode4Ctas8 : kDecodeCtas16), kDecThreads, smem, s, 1, a);
 }
 
 cudaError_t launch_kv4_decode(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
