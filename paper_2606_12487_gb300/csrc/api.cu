@@ -1000,7 +1000,7 @@ dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch
                            sinks, out_fp16, out_stride)) != DPTQ_OK)
     return st;
   const bool decode = (long long)a.k.c.max_tokens * a.group <= kDecodeRows;
-  DPTQ_CUDA(decode ? launch_kv4_decode(a, sc->num_sms, s) : launch_kv4_rows(a, sc->num_sms, s), "kv4_attention launch");
+  DPTQ_CUDA(decode ? launch_kv4_decode(a, sc->num_sms, s) : launch_kv4_prefill(a, sc->num_sms, s), "kv4_attention launch");
   return DPTQ_OK;
 }
 

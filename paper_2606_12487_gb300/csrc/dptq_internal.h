@@ -203,7 +203,7 @@ struct Kv4AttendArgs {
   int shortfall;
 };
 cudaError_t launch_kv4_decode(const Kv4AttendArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_kv4_rows(const Kv4AttendArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_kv4_prefill(const Kv4AttendArgs& a, int num_sms, cudaStream_t s);
 
 // ------------------------------------------------------------------ GEMM
 struct GemmArgs {

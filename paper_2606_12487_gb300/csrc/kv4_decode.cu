@@ -226,10 +226,10 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
       // a key's factor and addend, made by a lane for all
 #pragma unroll
       for (int k = lane; k < kKeys; k += 32) {
-        const float sk = bf16_float(ring.scale[stage][0][k]), sv = bf16_float(ring.scale[stage][1][k]);
-        const float v = fmaxf(sv, 0x1p-40f);   // (zeros, which add nothing)
+        const uint32_t sk = ring.scale[stage][0][k], sv = ring.scale[stage][1][k];
+        const float v = fmaxf(bf16_float(sv), 0x1p-40f);   // (zeros, which add nothing)
         // (NaN for a scale that is no number; what is not seen is masked below, so it stays with the rows that see it)
-        ring.factor[k] = make_float4(sk * unit, fmaf(sk + sv, 0.f, log2_fast(v)), rcp_fast(v), 0.f);
+        ring.factor[k] = make_float4(bf16_float(sk) * unit, kv4_bad(max(sk, sv)) ? NAN : log2_fast(v), rcp_fast(v), 0.f);
       }
       // logits of 16 keys and 8 rows: keys g, g + 8, rows 2 t, 2 t + 1
       float x[NG][RT][4];

@@ -8,6 +8,9 @@
 
 namespace dptq {
 
+// Scales are 0 to 9344, the largest that append makes of a finite value; anything else is no number (binary16 holds 7
+// times 9344).
+__device__ __forceinline__ bool kv4_bad(uint32_t scale_bits) { return scale_bits > 0x4612u; }
 __device__ __forceinline__ float bf16_float(uint16_t s) { return __uint_as_float((uint32_t)s << 16); }
 
 // Eight codes (two's complement nibbles of a word) to four pairs of binary16, in the order 0 4, 1 5, 2 6, 3 7.  A
