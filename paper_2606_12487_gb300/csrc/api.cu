@@ -956,7 +956,7 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
 namespace {
 dptq_status kv4_rows(const char* what, const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* k,
                      const void* v, long long stride, void* stream,
-                     cudaError_t (*launch)(const Kv4RowsArgs&, int, cudaStream_t)) {
+                     cudaError_t (*launch)(const Kv4RowsArgs&, cudaStream_t)) {
   NvtxRange nvtx_range(what);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   Kv4RowsArgs a{};
@@ -969,7 +969,7 @@ dptq_status kv4_rows(const char* what, const dptq_kv4_cache* cache, const dptq_k
   a.rows[0] = static_cast<__half*>(const_cast<void*>(k));
   a.rows[1] = static_cast<__half*>(const_cast<void*>(v));
   a.stride = stride;
-  DPTQ_CUDA(launch(a, sc->num_sms, s), what);
+  DPTQ_CUDA(launch(a, s), what);
   return DPTQ_OK;
 }
 }  // namespace

@@ -187,8 +187,8 @@ struct Kv4RowsArgs {
   __half* rows[2];       // K and V rows of the batch's tokens: read by append, written by read
   long long stride;
 };
-cudaError_t launch_kv4_append(const Kv4RowsArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_kv4_read(const Kv4RowsArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_kv4_append(const Kv4RowsArgs& a, cudaStream_t s);
+cudaError_t launch_kv4_read(const Kv4RowsArgs& a, cudaStream_t s);
 struct Kv4AttendArgs {
   Kv4Args k;
   const __half* q;       // as in Kv8AttendArgs

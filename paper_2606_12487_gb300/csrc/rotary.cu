@@ -51,7 +51,10 @@ __device__ __forceinline__ uint4 to_halves(const float (&f)[8]) {
 }
 
 // Whole units of 16 values: rot and head_dim are multiples of 16.  A CTA takes ROWS rows of a sequence and a part
-// (blockIdx.z) of their heads.
+// (blockIdx.z) of their heads, a thread one unit of every `side`-th head; the first kAhead of them are asked for before
+// the angles are made.
+constexpr int kAhead = 2;
+constexpr int kRotRows = 2, kRotFull = 8;
 template <int ROWS>
 __global__ void __launch_bounds__(kRotThreads) rotary_units_kernel(const RotaryArgs a) {
   __shared__ float cs[ROWS * kRotMost], sn[ROWS * kRotMost];
@@ -63,50 +66,67 @@ __global__ void __launch_bounds__(kRotThreads) rotary_units_kernel(const RotaryA
   const int first = max(-q.start, 0), row0 = first + blockIdx.x * ROWS;   // (rows at negative positions come first)
   if (row0 >= q.n) return;
   const int rows = min(ROWS, q.n - row0);
-  make_angles(a, q.start + row0, rows, cs, sn);
-  __syncthreads();
-  const int units = a.head_dim / 16, turned = a.rot / 16, all = turned + (a.x == a.out ? 0 : units - turned);
+  const int turned = a.rot / 16, all = a.x == a.out ? turned : a.head_dim / 16;   // units of a head that change; that are written
   const int r = threadIdx.x / kLane, at = threadIdx.x % kLane;
-  const int side = kLane / all;   // heads at a time
-  const int u = at % all, per = (a.heads + gridDim.z - 1) / gridDim.z, h0 = blockIdx.z * per, h1 = min(h0 + per, a.heads);
-  if (r >= rows || at >= side * all) return;
-  const size_t tok = (size_t)(q.tok0 + row0 + r);
+  const int side = kLane / all, u = at % all;   // heads side by side
+  const int per = (a.heads + gridDim.z - 1) / gridDim.z, h1 = min((blockIdx.z + 1) * per, a.heads);
+  int h = r < rows && at < side * all ? blockIdx.z * per + at / all : h1;
+  const size_t tok = (size_t)(q.tok0 + row0 + (r < rows ? r : 0));
   const __half* x = a.x + tok * a.x_stride;
   __half* y = a.out + tok * a.out_stride;
-  if (u >= turned) {   // the rest of a head
-    for (int h = h0 + at / all; h < h1; h += side) {
-      const int d = h * a.head_dim + 16 * u;
-      const uint4 v0 = ld_plain(reinterpret_cast<const uint4*>(x + d)), v1 = ld_plain(reinterpret_cast<const uint4*>(x + d) + 1);
-      *reinterpret_cast<uint4*>(y + d) = v0;
-      *(reinterpret_cast<uint4*>(y + d) + 1) = v1;
-    }
-    return;
+  // A unit: 8 pairs, or (u >= turned) 16 values of the rest of a head.
+  const bool near = a.interleaved || u >= turned;
+  const int d0 = near ? 16 * u : 8 * u, d1 = near ? d0 + 8 : d0 + a.rot / 2;
+  uint4 v0[kAhead], v1[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    // (threads without a head read the last one: a load in a branch would wait for its own data)
+    const int d = min(h + k * side, h1 - 1) * a.head_dim;
+    v0[k] = ld_plain(reinterpret_cast<const uint4*>(x + d + d0));
+    v1[k] = ld_plain(reinterpret_cast<const uint4*>(x + d + d1));
   }
+  make_angles(a, q.start + row0, rows, cs, sn);
+  __syncthreads();
   float c[8], s[8];
+  if (u < turned && r < rows) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    c[e] = cs[r * (a.rot / 2) + 8 * u + e];
-    s[e] = sn[r * (a.rot / 2) + 8 * u + e];
-  }
-  const int d0 = a.interleaved ? 16 * u : 8 * u, d1 = a.interleaved ? d0 + 8 : d0 + a.rot / 2;
-#pragma unroll 2
-  for (int h = h0 + at / all; h < h1; h += side) {
-    const int d = h * a.head_dim;
-    float f[8], g[8];
-    to_floats(ld_plain(reinterpret_cast<const uint4*>(x + d + d0)), f);
-    to_floats(ld_plain(reinterpret_cast<const uint4*>(x + d + d1)), g);
-    if (a.interleaved) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        turn_pair(f[2 * e], f[2 * e + 1], c[e], s[e]);
-        turn_pair(g[2 * e], g[2 * e + 1], c[4 + e], s[4 + e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) turn_pair(f[e], g[e], c[e], s[e]);
+    for (int e = 0; e < 8; ++e) {
+      c[e] = cs[r * (a.rot / 2) + 8 * u + e];
+      s[e] = sn[r * (a.rot / 2) + 8 * u + e];
     }
-    *reinterpret_cast<uint4*>(y + d + d0) = to_halves(f);
-    *reinterpret_cast<uint4*>(y + d + d1) = to_halves(g);
+  }
+  while (h < h1) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      uint4 w0 = v0[k], w1 = v1[k];
+      const int now = h + k * side;
+      if (now + kAhead * side < h1) {
+        const int d = (now + kAhead * side) * a.head_dim;
+        v0[k] = ld_plain(reinterpret_cast<const uint4*>(x + d + d0));
+        v1[k] = ld_plain(reinterpret_cast<const uint4*>(x + d + d1));
+      }
+      if (now >= h1) break;
+      if (u < turned) {
+        float f[8], g[8];
+        to_floats(w0, f);
+        to_floats(w1, g);
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            turn_pair(f[2 * e], f[2 * e + 1], c[e], s[e]);
+            turn_pair(g[2 * e], g[2 * e + 1], c[4 + e], s[4 + e]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) turn_pair(f[e], g[e], c[e], s[e]);
+        }
+        w0 = to_halves(f);
+        w1 = to_halves(g);
+      }
+      *reinterpret_cast<uint4*>(y + now * a.head_dim + d0) = w0;
+      *reinterpret_cast<uint4*>(y + now * a.head_dim + d1) = w1;
+    }
+    h += kAhead * side;
   }
 }
 
@@ -138,12 +158,21 @@ __global__ void __launch_bounds__(kRotThreads) rotary_pairs_kernel(const RotaryA
   }
 }
 
+template <int ROWS>
+static cudaError_t launch_units(const RotaryArgs& a, int parts, cudaStream_t s) {
+  return launch_after(rotary_units_kernel<ROWS>, dim3(ceil_div(a.c.max_tokens, ROWS), a.c.seqs, parts), kRotThreads, 0, s,
+                      1, a);
+}
+
 cudaError_t launch_rotary(const RotaryArgs& a, int num_sms, cudaStream_t s) {
-  const int n = a.c.max_tokens;
+  const long long rows = (long long)a.c.max_tokens * a.c.seqs;   // (most of them)
   if (a.rot % 16 != 0 || a.head_dim % 16 != 0)
-    return launch_after(rotary_pairs_kernel, dim3(n, a.c.seqs), kRotThreads, 0, s, 1, a);
-  const dim3 grid(n, a.c.seqs, 1);
-  return launch_after(rotary_units_kernel<1>, grid, kRotThreads, 0, s, 1, a);
+    return launch_after(rotary_pairs_kernel, dim3(a.c.max_tokens, a.c.seqs), kRotThreads, 0, s, 1, a);
+  if (a.c.max_tokens >= kRotRows && rows >= (long long)kRotRows * kRotFull * num_sms) return launch_units<kRotRows>(a, 1, s);
+  // Few rows: their heads over as many CTAs as there are SMs, while a thread has more than it asks for ahead.
+  long long parts = ceil_div((long long)a.heads * (a.head_dim / 16), kAhead * kRotThreads);
+  if (parts > num_sms / rows) parts = num_sms / rows;
+  return launch_units<1>(a, parts > 1 ? (int)parts : 1, s);
 }
 
 }  // namespace dptq
