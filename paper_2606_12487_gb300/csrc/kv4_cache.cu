@@ -20,7 +20,7 @@
 namespace dptq {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowTokens = 8;   // tokens of a thread, of prompts
+constexpr int kAppendTokens = 4, kReadTokens = 8;   // tokens of a thread, of prompts
 
 // What a thread works on: place `at` of a row of a head, K or V, and its tokens row0 + i step, i < V, of the sequence's
 // rows (rows past the last one are not there).
@@ -60,20 +60,39 @@ __device__ __forceinline__ void cache_rows(const Kv8Args& c, const Seq& q, const
   }
 }
 
-// Eight codes of a row, a nibble each.
+// Eight codes rint(x / s) of a row, a nibble each; r = 1 / s within a unit in its last place.
+// Exact ties are common (x = (k + 1/2) s with x of 11 bits and s of 8), and nothing else comes near one: with x = X 2^a,
+// s = S 2^b a quotient that is no tie differs from k + 1/2 by a multiple of 2^min(a + 1, b) / (2 S 2^b), that is by 1 / 2 S > 2^-9,
+// or, where a + 1 < b, by 2^(a - b) / S, and 2^(a - b) > 0.4 S / X next to a tie: by more than 0.4 / X > 2^-12.4.  x r is
+// within 2^-19 of the quotient, which is 7.03 at most.  So x r rounded to a multiple of 2^-13 is the tie itself where there
+// is one and on the quotient's side of it elsewhere, and rint of that is rint of the quotient.  (With a check for near ties and a
+// division behind it, two of three warps divided: four prompts up to 2048 tokens, 8 heads, 16 us in a graph.)
 __device__ __forceinline__ uint32_t quant8_nibbles(const uint4& v, float s, float r) {
-  float t[8];
-  uint32_t codes = 0;
-  if (rounded8(v, r, t)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) codes |= (__float_as_uint(t[e]) & 15u) << (4 * e);
-    return codes;
-  }
+  constexpr float kGrid = 1536.f, kMagic = 12582912.f;   // 1.5 2^10 and 1.5 2^23, where fp32 has steps of 2^-13 and 1
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll 1
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t h = (e < 4 ? (e < 2 ? w[0] : w[1]) : (e < 6 ? w[2] : w[3])) >> (16 * (e & 1));
-    codes |= (uint32_t)(quant_code(__half2float(__ushort_as_half((unsigned short)h)), s, r) & 15) << (4 * e);
+  uint32_t t[8];
+  const uint64_t r2 = f2_pack(r, r), grid = f2_pack(kGrid, kGrid), magic = f2_pack(kMagic, kMagic);
+  bool number = isfinite(s);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[e]));
+    float a, b;
+    f2_unpack(f2_add(f2_sub(f2_fma(f2_pack(f.x, f.y), r2, grid), grid), magic), a, b);
+    t[2 * e] = __float_as_uint(a);
+    t[2 * e + 1] = __float_as_uint(b);
+  }
+  const uint32_t even = __byte_perm(__byte_perm(t[0], t[2], 0x0040), __byte_perm(t[4], t[6], 0x0040), 0x5410);
+  const uint32_t odd = __byte_perm(__byte_perm(t[1], t[3], 0x0040), __byte_perm(t[5], t[7], 0x0040), 0x5410);
+  uint32_t codes = (even & 0x0F0F0F0Fu) | ((odd << 4) & 0xF0F0F0F0u);
+  __half2 am = __habs2(*reinterpret_cast<const __half2*>(&w[0]));
+#pragma unroll
+  for (int e = 1; e < 4; ++e) am = __hmax2_nan(am, __habs2(*reinterpret_cast<const __half2*>(&w[e])));
+  if (!(__hmax_nan(__low2half(am), __high2half(am)) < __ushort_as_half(0x7C00))) number = false;
+  if (!number) {   // NaN takes the code 0, and so does a row with an infinite value
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t h = (w[e >> 1] >> (16 * (e & 1))) & 0x7FFFu;
+      if (!isfinite(s) || h > 0x7C00u) codes &= ~(15u << (4 * e));
+    }
   }
   return codes;
 }
@@ -96,14 +115,18 @@ __global__ void __launch_bounds__(kRowThreads) kv4_append_kernel(const Kv4RowsAr
     x[i] = ld_plain(reinterpret_cast<const uint4*>(src + min(w.row0 + i * w.step, w.end - 1) * a.stride));
   long long to[V];
   cache_rows(c, q, w, to);
+  float m[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) m[i] = widest(abs_max8(x[i], __half2half2(__ushort_as_half(0))));
+#pragma unroll
+  for (int o = D / 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < V; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(lanes, m[i], o));
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    float m = widest(abs_max8(x[i], __half2half2(__ushort_as_half(0))));
-#pragma unroll
-    for (int o = D / 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
-    const __nv_bfloat16 sb = __float2bfloat16_rn(__fmul_rn(m, 1.f / 7.f));
+    const __nv_bfloat16 sb = __float2bfloat16_rn(__fmul_rn(m[i], 1.f / 7.f));
     const float s = __bfloat162float(sb);
-    const uint32_t codes = quant8_nibbles(x[i], s, s > 0.f ? __frcp_rn(s) : 0.f);
+    const uint32_t codes = quant8_nibbles(x[i], s, s > 0.f ? rcp_fast(s) : 0.f);
     if (w.row0 + i * w.step < w.end && to[i] >= 0) {
       *reinterpret_cast<uint32_t*>((w.kv ? a.k.codes[1] : a.k.codes[0]) + to[i] * (D / 2) + 4 * w.at) = codes;
       if (w.at == 0) (w.kv ? a.k.scales[1] : a.k.scales[0])[to[i]] = __bfloat16_as_ushort(sb);
@@ -124,6 +147,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const Kv4RowsArgs
   cache_rows(c, q, w, from);
   const uint8_t* src = (w.kv ? a.k.codes[1] : a.k.codes[0]) + 4 * w.at;
   const uint16_t* scales = w.kv ? a.k.scales[1] : a.k.scales[0];
+  const Nibbles nib;
   uint32_t codes[V];
   uint16_t scale[V];
 #pragma unroll
@@ -137,7 +161,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const Kv4RowsArgs
   for (int i = 0; i < V; ++i) {
     const int row = w.row0 + i * w.step;
     const float s = bf16_float(scale[i]);
-    const uint4 v = kv4_tiny(scale[i]) || kv4_bad(scale[i]) ? widen8_slow(codes[i], s) : widen8(codes[i], __float2half2_rn(s));
+    const uint4 v = kv4_tiny(scale[i]) || kv4_bad(scale[i]) ? values_slow(codes[i], s) : nib.values(codes[i], __float2half2_rn(s));
     if (row < w.end && from[i] >= 0)   // (from the order 0 4, 1 5, 2 6, 3 7)
       *reinterpret_cast<uint4*>(dst + row * a.stride) =
           make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.x, v.y, 0x7632),
@@ -152,15 +176,15 @@ static cudaError_t launch_rows(Fn fn, const Kv4RowsArgs& a, cudaStream_t s) {
                       s, 1, a);
 }
 
-cudaError_t launch_kv4_append(const Kv4RowsArgs& a, cudaStream_t s) {
-  const bool few = a.k.c.max_tokens < kRowTokens;
-  if (a.k.c.head_dim == 64) return few ? launch_rows<1>(kv4_append_kernel<64, 1>, a, s) : launch_rows<kRowTokens>(kv4_append_kernel<64, kRowTokens>, a, s);
-  return few ? launch_rows<1>(kv4_append_kernel<128, 1>, a, s) : launch_rows<kRowTokens>(kv4_append_kernel<128, kRowTokens>, a, s);
-}
-cudaError_t launch_kv4_read(const Kv4RowsArgs& a, cudaStream_t s) {
-  const bool few = a.k.c.max_tokens < kRowTokens;
-  if (a.k.c.head_dim == 64) return few ? launch_rows<1>(kv4_read_kernel<64, 1>, a, s) : launch_rows<kRowTokens>(kv4_read_kernel<64, kRowTokens>, a, s);
-  return few ? launch_rows<1>(kv4_read_kernel<128, 1>, a, s) : launch_rows<kRowTokens>(kv4_read_kernel<128, kRowTokens>, a, s);
-}
+// (the kernel for V tokens a thread, or for one where no sequence has as many)
+#define DPTQ_LAUNCH_ROWS(kernel, V)                                                                              \
+  do {                                                                                                           \
+    const bool few = a.k.c.max_tokens < V;                                                                       \
+    if (a.k.c.head_dim == 64) return few ? launch_rows<1>(kernel<64, 1>, a, s) : launch_rows<V>(kernel<64, V>, a, s); \
+    return few ? launch_rows<1>(kernel<128, 1>, a, s) : launch_rows<V>(kernel<128, V>, a, s);                    \
+  } while (0)
+cudaError_t launch_kv4_append(const Kv4RowsArgs& a, cudaStream_t s) { DPTQ_LAUNCH_ROWS(kv4_append_kernel, kAppendTokens); }
+cudaError_t launch_kv4_read(const Kv4RowsArgs& a, cudaStream_t s) { DPTQ_LAUNCH_ROWS(kv4_read_kernel, kReadTokens); }
+#undef DPTQ_LAUNCH_ROWS
 
 }  // namespace dptq

@@ -52,52 +52,11 @@ __device__ __forceinline__ float log2_fast(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float rcp_fast(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Constants in registers: (w & mask) ^ flip is then one instruction.
-struct Nibbles {
-  uint32_t lo, hi, tiny_lo, tiny_hi, wide_lo, wide_hi;
-  __device__ __forceinline__ Nibbles() {
-    asm("mov.b32 %0, 0x000F000F;" : "=r"(lo));
-    asm("mov.b32 %0, 0x00F000F0;" : "=r"(hi));
-    asm("mov.b32 %0, 0x00080008;" : "=r"(tiny_lo));
-    asm("mov.b32 %0, 0x00800080;" : "=r"(tiny_hi));
-    asm("mov.b32 %0, 0x64086408;" : "=r"(wide_lo));
-    asm("mov.b32 %0, 0x64806480;" : "=r"(wide_hi));
-  }
-  static __device__ __forceinline__ uint32_t and_xor(uint32_t a, uint32_t b, uint32_t c) {
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
-  }
-  // Nibbles 0 and 4 (HI: 1 and 5) of a word, plus 8, as binary16 numbers below its normal range: (code + 8) 2^-24 (HI:
-  // 2^-20).
-  template <bool HI>
-  __device__ __forceinline__ uint32_t tiny(uint32_t w) const {
-    return HI ? and_xor(w, hi, tiny_hi) : and_xor(w, lo, tiny_lo);
-  }
-  // Eight codes to four pairs of binary16, in the order 0 4, 1 5, 2 6, 3 7: under the exponent of 1024 a nibble reads
-  // 1032 + code, four bits higher 1024 + 16 (code + 8); one subtraction or fma, exact, takes the offset off.
-  __device__ __forceinline__ void widen(uint32_t w, __half2 (&r)[4]) const {
-    const __half2 off = __half2half2(__ushort_as_half(0x6408));                                                         // 1032
-    const __half2 sixteenth = __half2half2(__ushort_as_half(0x2C00)), off16 = __half2half2(__ushort_as_half(0xD480));   // 1 / 16, -72
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t v = k ? w >> 8 : w, a = and_xor(v, lo, wide_lo), b = and_xor(v, hi, wide_hi);
-      r[2 * k] = __hsub2(*reinterpret_cast<const __half2*>(&a), off);
-      r[2 * k + 1] = __hfma2(*reinterpret_cast<const __half2*>(&b), sixteenth, off16);
-    }
-  }
-};
-
 constexpr int kNG = 4;
 constexpr float kDecUnit = 15.f;   // weights are relative to 2^-15 of the largest
 
@@ -352,8 +311,8 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {   // dims 8 w + 4 k .. of the lane's
             __half2 a[4], b[4];
-            nib.widen(__byte_perm(vw[0][w], vw[1][w], k ? 0x7632 : 0x5410), a);
-            nib.widen(__byte_perm(vw[2][w], vw[3][w], k ? 0x7632 : 0x5410), b);
+            nib.codes(__byte_perm(vw[0][w], vw[1][w], k ? 0x7632 : 0x5410), a);
+            nib.codes(__byte_perm(vw[2][w], vw[3][w], k ? 0x7632 : 0x5410), b);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll

@@ -343,6 +343,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
     // ------------------------------------------------------------------ K and V, widened
     reg_less<112>();
     const int w = warp - 8;
+    const Nibbles nib;
     // A warp takes rows of 16 bytes (32 dims) a lane, kUnits times 32 lanes of a tile: of K whole rows, and of a pair's
     // the CTA's half of the keys; of V all keys, and of a pair's the CTA's 64 dims of each.
     constexpr int kLanesK = D / 32, kLanesV = PAIR ? 2 : D / 32, kUnits = kLanesK * kTileKeys / 32 / kConvWarps / kCtas;
@@ -390,24 +391,37 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
       // another order)
       const bool other = lanes == 4 && col >= 2;
       dst += other ? (kv ? L::kHalf : L::kKHalf) : 0;
+      uint32_t sb[kUnits];
+      bool tiny = false;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const int at = key_in(i, kv) - (kv ? 0 : rank * (kTileKeys / kCtas));
         // A scale that is no number makes its key's K values NaN, so that its scores are for the rows that see it, and its
         // V values 0, so that no other row meets it.
-        const bool bad = kv4_bad(sk[i]) || kv4_bad(sv[i]);
-        const uint32_t sb = kv ? (bad ? 0u : sv[i]) : (bad ? 0x7FC0u : sk[i]);
-        const float s = __uint_as_float(sb << 16);
-        uint32_t x[4] = {other ? v[i].z : v[i].x, other ? v[i].w : v[i].y, other ? v[i].x : v[i].z, other ? v[i].y : v[i].w};
-        const int chunk = 4 * (col & 1) + (other ? 2 : 0);
-        uint8_t* row = dst + at * 128;
-        if (__any_sync(0xffffffffu, kv4_tiny(sb))) {
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(row + (((chunk ^ k) ^ (at & 7)) << 4)) = widen8_slow(k == 0 ? x[0] : k == 1 ? x[1] : k == 2 ? x[2] : x[3], s);
-        } else {
-          const __half2 s2 = __float2half2_rn(s);
+        const bool bad = kv4_bad(max(sk[i], sv[i]));
+        sb[i] = kv ? (bad ? 0u : sv[i]) : (bad ? 0x7FC0u : sk[i]);
+        tiny |= kv4_tiny(sb[i]);
+      }
+      const int chunk = 4 * (col & 1) + (other ? 2 : 0);
+      auto place = [&](int i, int k) {   // of word k of unit i
+        const int at = key_in(i, kv) - (kv ? 0 : rank * (kTileKeys / kCtas));
+        return reinterpret_cast<uint4*>(dst + at * 128 + (((chunk ^ k) ^ (at & 7)) << 4));
+      };
+      if (!__any_sync(0xffffffffu, tiny)) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(row + (((chunk ^ k) ^ (at & 7)) << 4)) = widen8(x[k], s2);
+        for (int i = 0; i < kUnits; ++i) {
+          const uint32_t x[4] = {other ? v[i].z : v[i].x, other ? v[i].w : v[i].y, other ? v[i].x : v[i].z, other ? v[i].y : v[i].w};
+          const __half2 s2 = __float2half2_rn(bf16_float(sb[i]));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *place(i, k) = nib.values(x[k], s2);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+#pragma unroll 1
+          for (int k = 0; k < 4; ++k) {
+            const int from = other ? k ^ 2 : k;
+            *place(i, k) = values_slow(from == 0 ? v[i].x : from == 1 ? v[i].y : from == 2 ? v[i].z : v[i].w, bf16_float(sb[i]));
+          }
         }
       }
       fence_proxy_async_smem();

@@ -37,11 +37,25 @@ __device__ __forceinline__ uint2 pack_codes(const int (&c)[8]) {
   for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)(c[e] & 0xFF) << (8 * (e & 3));
   return make_uint2(w[0], w[1]);
 }
-// Eight codes as quant_code makes them.
+// Eight codes as quant_code makes them, two values an instruction: t = x r + 1.5 2^23 holds
+// rint(x r) in its low byte, and x r - rint(x r), from one fma, says whether the quotient itself has to
+// decide (or a NaN has turned up).  One value at a time took 12.0 us in a graph for four prompts
+// (39.6 MB), this takes 9.4 us.
 __device__ __forceinline__ uint2 quant8(const uint4& v, float s, float r) {
-  float t[8];
-  if (!rounded8(v, r, t)) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  constexpr float kMagic = 12582912.f;   // 1.5 2^23
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  const uint64_t r2 = f2_pack(r, r), magic = f2_pack(kMagic, kMagic), n2 = f2_pack(-r, -r);
+  float t[8], d = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[e]));
+    const uint64_t x2 = f2_pack(f.x, f.y), t2 = f2_fma(x2, r2, magic);
+    float d0, d1;
+    f2_unpack(f2_fma(x2, n2, f2_sub(t2, magic)), d0, d1);   // rint(x r) - x r
+    asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(d) : "f"(fabsf(d0)), "f"(fabsf(d1)));
+    f2_unpack(t2, t[2 * e], t[2 * e + 1]);
+  }
+  if (!(d < 0.5f - 0x1p-15f)) {
     int c[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {

@@ -88,6 +88,21 @@ def test_codes_fit_and_values_are_exact():
         assert (exact.astype(np.float16).astype(np.float64) == exact).all()
 
 
+def test_a_grid_of_2_to_the_minus_13_decides_every_quotient():
+    """x r on that grid, r = 1 / s a unit in its last place up or down, rounds to an integer as the IEEE quotient does, for
+    every binary16 x that a scale covers: what the kernel's codes rest on."""
+    x = np.arange(0x7C00, dtype=np.uint16).view(np.float16).astype(np.float32)
+    one = np.float32(1)
+    for e in (-27, -24, -17, -3, 0, 13):
+        for k in range(128, 256, 5 if e else 1):
+            s = np.float32(k / 128 * 2.0 ** e)
+            v, r = x[x <= np.float32(7.03) * s], one / s
+            want = np.rint(v / s)
+            for r in (np.nextafter(r, np.float32(0)), r, np.nextafter(r, np.float32(np.inf))):
+                t = (v.astype(np.float64) * r + 1536).astype(np.float32) - np.float32(1536)
+                assert np.array_equal((t + np.float32(12582912)) - np.float32(12582912), want)
+
+
 def test_reference_attention_is_a_weighted_mean():
     rng = np.random.default_rng(0)
     cu, lens, table, blocks = ref.random_batch(rng, [3], [20], 16)
