@@ -155,10 +155,10 @@ constexpr int kDecodeRows = 16;
 // Decode grids: CTAs an SM for up to 8 and up to 16 rows; each CTA leaves partial results of two
 // (sequence, head)s at most: weighted values, maximum and sum of each row.
 constexpr int kDecodeCtas8 = 3, kDecodeCtas16 = 2, kDecode4Ctas8 = 3;   // (kDecode4Ctas8: of the 4-bit cache)
-// A prompt's grid that is split along the keys has at most a CTA an SM, of 256 rows.
+// A prompt's grid that is split along the keys has at most a CTA an SM, of 256 rows (of the 4-bit cache: two).
 inline size_t kv8_ws_bytes(int num_sms) {
-  const int r8 = 2 * kDecodeCtas8 * 8, r16 = 2 * kDecodeCtas16 * 16, r = r8 > r16 ? r8 : r16;
-  return (size_t)num_sms * (r > 256 ? r : 256) * (128 + 2) * sizeof(float);
+  static_assert(2 * kDecodeCtas8 * 8 <= 512 && 2 * kDecodeCtas16 * 16 <= 512 && 2 * kDecode4Ctas8 * 8 <= 512, "rows of an SM");
+  return (size_t)num_sms * 512 * (128 + 2) * sizeof(float);
 }
 inline size_t kv8_counter_words(int num_sms) { return (size_t)num_sms * 4 * 3; }
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, int num_sms, cudaStream_t s);

@@ -13,11 +13,14 @@
 //
 // Warp roles: 0-3 and 4-7 softmax and output of the row tiles, a row a thread; 8-11 widen K and
 // V tiles (global to registers a tile ahead, then to shared memory in the 128-byte swizzle);
-// 12 issues the MMAs.  Many rows (kPairRows): pairs of CTAs, each widening half of every tile (PAIR below).  Few row
-// tiles are split along the keys: each CTA leaves its rows' sums, and a second launch joins them.
+// 12 issues the MMAs.  Many rows (kPairRows): pairs of CTAs, each widening half of every tile (PAIR below).
+//
+// A task is the 256 rows (512 of a pair) of one (sequence, KV head).  Tasks that would leave SMs without work in the
+// last wave are split along the keys (Cut): each CTA leaves its rows' sums, and a second launch joins them.
 //
 // The order of the dims: a word of eight nibbles widens to the pairs (0, 4), (1, 5), (2, 6), (3, 7).  q is stored in
 // that order too, and the output's registers are written from it.
+#include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
@@ -29,12 +32,17 @@ namespace dptq {
 
 constexpr float kUnit = 7.f;   // weights are relative to 2^-7 of the largest
 
+// Where the rows of a CTA or pair go: slot of the scratch for a part of a task's keys, -1 for whole tasks.
+struct Out {
+  int tok0, row0, nrows, head, slot;
+};
 struct Pre4Shared {
   uint64_t kfull[kPreStages], kempty[kPreStages], vfull[kPreStages], vempty[kPreStages];
   uint64_t mfull[kMeta];   // `gone` is there (filled and read within a CTA)
   uint64_t qfull[2], sfull[2], pfull[2][2], ofull[2], drain;   // pfull: the two halves of a tile's keys
   uint64_t phalf[2];   // the first half's product is complete
   uint32_t gone[kMeta];   // bit g: no page for the tile's keys 16 g ..
+  Out out;
   uint32_t tmem;
   int abort;
 };
@@ -75,7 +83,60 @@ __device__ __forceinline__ bool wait_two(uint64_t* b0, uint32_t p0, uint64_t* b1
       abort_flag, err, code, limit);
 }
 
-// SPLIT: this CTA's part of the keys goes to the scratch, for kv4_join_kernel.
+// How the device cuts a call: all tasks, and those from `whole` on in `parts` parts of their keys each.
+struct Cut {
+  int tasks, whole, parts;
+};
+// Whole waves of tasks stay whole.  The r tasks behind them, where they are fewer than the P that run at a time, are cut
+// into floor(P / r) parts, or, from P / 2 to 2 P / 3, into three (two shorter waves); most: the host's bound, 1 for calls whose last wave is
+// a small part of them.
+__device__ __forceinline__ Cut cut_tasks(int tasks, int P, int most) {
+  Cut r{tasks, tasks, 1};
+  if (most < 2) return r;
+  const int left = tasks % P;
+  if (left == 0) return r;
+  int parts = P / left;
+  if (parts < 2 && 3 * left <= 2 * P) parts = 3;
+  if (parts > most) parts = most;
+  if (parts > 1) r.whole = tasks - left, r.parts = parts;
+  return r;
+}
+// A task: a sequence, a KV head, and the number of its row tile counted from the sequence's last one, which sees the most
+// keys; tasks are taken in the order of that number, so that long ones come first, then of sequences and heads.
+struct Task {
+  int seq, head, from_last;
+};
+constexpr int kFewSeqs = 32;   // sequences that a warp knows the tiles of
+// The part `index` of a call of at most kFewSeqs sequences: its task, which of the task's parts it is, and how the call is
+// cut; false past the last one.  Every warp finds it by itself.  All results come out of shuffles and votes: the compiler
+// then knows that they are the same in a warp, and loops that it takes to be divergent would cost a prompt of 8192 tokens
+// 160 us.
+__device__ __forceinline__ bool find_task(const Kv8Args& c, int group, int rows, int index, int P, int most, bool tells, Cut& cut,
+                                          Task& task, int& part) {
+  const int lane = threadIdx.x & 31;
+  Seq q;
+  const int mine = lane < c.seqs && load_seq(c, lane, q, tells) ? (q.n * group + rows - 1) / rows : 0;
+  cut = cut_tasks(__reduce_add_sync(0xffffffffu, mine) * c.kv_heads, P, most);
+  int u = index;
+  part = 0;
+  if (u >= cut.whole) {
+    u = cut.whole + (index - cut.whole) / cut.parts;
+    part = (index - cut.whole) % cut.parts;
+  }
+  if (u >= cut.tasks) return false;
+  task.head = u % c.kv_heads;
+  const int tile = u / c.kv_heads;
+  // the largest z of which min(tiles, z) over all sequences make at most `tile`
+  int z = 0;
+  for (int step = 1 << (31 - __clz(__reduce_max_sync(0xffffffffu, mine))); step > 0; step >>= 1)
+    if (__reduce_add_sync(0xffffffffu, min(mine, z + step)) <= tile) z += step;
+  const uint32_t there = __ballot_sync(0xffffffffu, mine > z);
+  const int k = tile - __reduce_add_sync(0xffffffffu, min(mine, z));
+  task.from_last = z;
+  task.seq = __ffs(__ballot_sync(0xffffffffu, (there >> lane & 1u) && __popc(there & ((1u << lane) - 1)) == k)) - 1;
+  return true;
+}
+
 // PAIR: two CTAs of a cluster work on 512 rows, 256 each; the tensor cores of both take K and V
 // tiles of which each CTA widens and holds one half (of K's keys, of V's dims).  That halves the
 // widening, its stores and what the MMAs read of K and V from shared memory, which is what a
@@ -83,9 +144,10 @@ __device__ __forceinline__ bool wait_two(uint64_t* b0, uint32_t p0, uint64_t* b1
 // its barriers in three ways: q, once, released at cluster scope; K and V on the second CTA's own
 // barriers, from which its MMA warp, which has no loads under way, passes them on released at cluster
 // scope; P, stores to tensor memory, as mbar_arrive_remote says.
-template <int D, bool SPLIT, bool PAIR>
-__global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4AttendArgs A, int nsplit) {
-  static_assert(!PAIR || (D == 128 && !SPLIT), "a pair's halves of V are 64 dims; few rows take no pairs");
+// CUT: tasks may be cut (P, most: cut_tasks); otherwise the grid is KV heads x sequences x row tiles.
+template <int D, bool PAIR, bool CUT>
+__global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4AttendArgs A, int P, int most) {
+  static_assert(!PAIR || D == 128, "a pair's halves of V are 64 dims");
   using L = PreLayout<D, PAIR, (int)sizeof(Pre4Shared)>;
   constexpr int kCtas = PAIR ? 2 : 1, kRows = kCtas * 2 * kTileRows;   // rows of a CTA or pair
   extern __shared__ uint8_t raw[];
@@ -93,22 +155,34 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
   Pre4Shared& S = *reinterpret_cast<Pre4Shared*>(sm + L::kEnd);
   const Kv8Args& c = A.k.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int head = blockIdx.x / kCtas, rank = PAIR ? blockIdx.x & 1 : 0, seq = blockIdx.y;
-  const int split = SPLIT ? blockIdx.z % nsplit : 0, zt = SPLIT ? blockIdx.z / nsplit : blockIdx.z;
+  const int rank = PAIR ? blockIdx.x & 1 : 0;
   pdl_launch_dependents();
   pdl_wait();
+  Cut cut;
+  Task task;
+  int part;
+  const int index = blockIdx.x / kCtas;
+  if constexpr (CUT) {
+    if (!find_task(c, A.group, kRows, index, P, most, blockIdx.x == 0 && warp == 0, cut, task, part)) return;
+  } else {
+    task = {(int)blockIdx.y, index, (int)blockIdx.z};
+  }
+  const int seq = task.seq, head = task.head;
+  const bool split = CUT && index >= cut.whole;
   Seq q;
-  if (!load_seq(c, seq, q, tid == 0 && blockIdx.z == 0 && head == 0)) return;
+  if (!load_seq(c, seq, q, !CUT && tid == 0 && head == 0 && blockIdx.z == 0)) return;
   const int rows = q.n * A.group;
-  const int tile = (rows + kRows - 1) / kRows - 1 - zt;   // the last rows, with the most keys, first
-  if (tile < 0) return;
+  const int tile = (rows + kRows - 1) / kRows - 1 - task.from_last;
+  if (!CUT && tile < 0) return;
   const int row0 = tile * kRows, nrows = rows - row0 < kRows ? rows - row0 : kRows;
   const int halves = nrows > kCtas * kTileRows ? 2 : 1;   // row tiles (of a pair: 256 rows)
   const int p_first = q.start + row0 / A.group, p_last = q.start + (row0 + nrows - 1) / A.group;
   const Tiles all = row_tiles(p_first, p_last, A.window, A.sinks);
-  const int j0 = SPLIT ? (int)((long long)all.count * split / nsplit) : 0;
-  const int nt = (SPLIT ? (int)((long long)all.count * (split + 1) / nsplit) : all.count) - j0;
+  // (at most 2^20 tiles and 256 parts)
+  const int j0 = split ? (int)((unsigned)all.count * part / (unsigned)cut.parts) : 0;
+  const int nt = (split ? (int)((unsigned)all.count * (part + 1) / (unsigned)cut.parts) : all.count) - j0;
 
+  if (CUT && tid == 0) S.out = {q.tok0, row0, nrows, head, split ? index - cut.whole : -1};
   if (tid == 0) {
     for (int i = 0; i < kPreStages; ++i) {
       mbar_init(&S.kfull[i], (A.shortfall == 1) + kConvWarps + (PAIR && rank == 0 ? 1 : 0));   // (and the second CTA's MMA warp)
@@ -163,8 +237,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
     const uint32_t tlane = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tm + tlane + t * 128, tO = tm + tlane + 256 + t * 128;
     float m = -INFINITY, l = 0.f;
-    const float unit = fmaxf(fabsf(A.scale) * 1.4426950408889634f, 1e-37f);   // (above 0: a masked -inf stays)
     bool ok = true;
+    const float unit = fmaxf(fabsf(A.scale) * 1.4426950408889634f, 1e-37f);   // (above 0: a masked -inf stays)
     if (t < halves && nt > 0) {
       {   // the warp's rows of q, whole rows at a time, in the order of the dims that a widened word has, negated for a
           // negative scale
@@ -297,20 +371,28 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
       if (ok) ok = wait_one(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
       tc_fence_after();
     }
-    // ---- output (the accumulators of a chunk of 8 dims stand in the order 0 4 1 5 2 6 3 7)
+    // ---- output (the accumulators of a chunk of 8 dims stand in the order 0 4 1 5 2 6 3 7); of a call that is cut, where it
+    // goes comes from shared memory, since registers for it would be missing in the loop
     if (ok && t < halves) {
-      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
-      __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D;
-      float* part = nullptr;
-      if constexpr (SPLIT) {
-        part = A.ws + ((((size_t)seq * (gridDim.z / nsplit) + tile) * gridDim.x + head) * nsplit + split) *
-                          (2 * kTileRows * (D + 2));
-        if (mine) {
-          part[2 * kTileRows * D + t * kTileRows + r] = m;
-          part[2 * kTileRows * (D + 1) + t * kTileRows + r] = l;
-        }
-        part += (size_t)(t * kTileRows + r) * D;
+      Out w{q.tok0, row0, nrows, head, -1};
+      if constexpr (CUT) {
+        volatile const Out& v = S.out;
+        w = {v.tok0, v.row0, v.nrows, v.head, v.slot};
       }
+      const int at = (t * kCtas + rank) * kTileRows + r, row = w.row0 + at;
+      const bool mine = at < w.nrows, sums_only = CUT && w.slot >= 0;
+      float* sums = nullptr;
+      if (sums_only) {   // weighted values [kRows][D], then maxima, then sums
+        sums = A.ws + (size_t)w.slot * (kRows * (D + 2));
+        if (mine) {
+          sums[kRows * D + at] = m;
+          sums[kRows * (D + 1) + at] = l;
+        }
+        sums += (size_t)at * D;
+      }
+      const float inv = l == 0.f ? 0.f : __frcp_rn(l);
+      const int tok = row / A.group, hh = row - tok * A.group;
+      __half* dst = A.out + (size_t)(w.tok0 + tok) * A.out_stride + (size_t)(w.head * A.group + hh) * D;
 #pragma unroll
       for (int k = 0; k < D; k += 32) {
         float o[32];
@@ -321,19 +403,18 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
-        if (mine) {
-          if constexpr (SPLIT) {
+        if (mine && !sums_only) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              *reinterpret_cast<float4*>(part + k + e) = make_float4(o[e], o[e + 2], o[e + 4], o[e + 6]);
-              *reinterpret_cast<float4*>(part + k + e + 4) = make_float4(o[e + 1], o[e + 3], o[e + 5], o[e + 7]);
-            }
-          } else {
+          for (int e = 0; e < 32; e += 8)
+            *reinterpret_cast<uint4*>(dst + k + e) =
+                make_uint4(pack_half2(o[e] * inv, o[e + 2] * inv), pack_half2(o[e + 4] * inv, o[e + 6] * inv),
+                           pack_half2(o[e + 1] * inv, o[e + 3] * inv), pack_half2(o[e + 5] * inv, o[e + 7] * inv));
+        }
+        if (mine && sums_only) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              *reinterpret_cast<uint4*>(dst + k + e) =
-                  make_uint4(pack_half2(o[e] * inv, o[e + 2] * inv), pack_half2(o[e + 4] * inv, o[e + 6] * inv),
-                             pack_half2(o[e + 1] * inv, o[e + 3] * inv), pack_half2(o[e + 5] * inv, o[e + 7] * inv));
+          for (int e = 0; e < 32; e += 8) {
+            *reinterpret_cast<float4*>(sums + k + e) = make_float4(o[e], o[e + 2], o[e + 4], o[e + 6]);
+            *reinterpret_cast<float4*>(sums + k + e + 4) = make_float4(o[e + 1], o[e + 3], o[e + 5], o[e + 7]);
           }
         }
       }
@@ -565,19 +646,27 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
   }
 }
 
-// Joins the parts of the keys: a warp a row.
+// Joins the parts of the keys of the tasks that were cut (blockIdx.y counts them): a warp a row.
+constexpr int kJoinThreads = 256;
 template <int D>
-__global__ void __launch_bounds__(256) kv4_join_kernel(const Kv4AttendArgs A, int nsplit, int tiles) {
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, head = blockIdx.y, seq = blockIdx.z;
+__global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(const Kv4AttendArgs A, int rows, int P, int most) {
+  const int r = blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const Kv8Args& c = A.k.c;
   pdl_launch_dependents();
   pdl_wait();
+  Cut cut;
+  Task task;
+  int part;
+  if (!find_task(c, A.group, rows, 0, P, most, false, cut, task, part) || cut.whole + (int)blockIdx.y >= cut.tasks) return;
+  find_task(c, A.group, rows, cut.whole + blockIdx.y * cut.parts, P, most, false, cut, task, part);
   Seq q;
-  if (!load_seq(A.k.c, seq, q, false) || row >= q.n * A.group) return;
-  const int tile = row / (2 * kTileRows), r = row % (2 * kTileRows);
-  constexpr size_t kPart = 2 * kTileRows * (D + 2);
-  const float* part = A.ws + (((size_t)seq * tiles + tile) * gridDim.y + head) * nsplit * kPart;
+  load_seq(c, task.seq, q, false);
+  const int n = q.n * A.group, row = ((n + rows - 1) / rows - 1 - task.from_last) * rows + r;
+  if (row >= n) return;
+  const size_t pitch = (size_t)rows * (D + 2);
+  const float* sums = A.ws + (size_t)blockIdx.y * cut.parts * pitch;
   float M = -INFINITY;
-  for (int i = lane; i < nsplit; i += 32) M = fmaxf(M, __ldcg(part + i * kPart + 2 * kTileRows * D + r));
+  for (int k = lane; k < cut.parts; k += 32) M = fmaxf(M, __ldcg(sums + k * pitch + (size_t)rows * D + r));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   const float base = M == -INFINITY ? 0.f : M;
@@ -586,61 +675,60 @@ __global__ void __launch_bounds__(256) kv4_join_kernel(const Kv4AttendArgs A, in
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 4
-  for (int i = 0; i < nsplit; ++i) {
-    const float* p = part + i * kPart;
-    const float f = exp2_fast(__ldcg(p + 2 * kTileRows * D + r) - base);
-    l = fmaf(f, __ldcg(p + 2 * kTileRows * (D + 1) + r), l);
+  for (int k = 0; k < cut.parts; ++k) {
+    const float* p = sums + k * pitch;
+    const float f = exp2_fast(__ldcg(p + (size_t)rows * D + r) - base);
+    l = fmaf(f, __ldcg(p + (size_t)rows * (D + 1) + r), l);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldcg(p + (size_t)r * D + E * lane + e), o[e]);
   }
   const float inv = l == 0.f ? 0.f : __frcp_rn(l);
   const int tok = row / A.group, hh = row - tok * A.group;
-  __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(head * A.group + hh) * D + E * lane;
+  __half* dst = A.out + (size_t)(q.tok0 + tok) * A.out_stride + (size_t)(task.head * A.group + hh) * D + E * lane;
 #pragma unroll
   for (int e = 0; e < E; e += 2) *reinterpret_cast<__half2*>(dst + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
 }
 
 // Rows of a sequence and KV head from which pairs of CTAs take them.
 constexpr int kPairRows = 512;
+// Calls of so many waves are not cut, since their tasks do not end together, and calls whose last tasks have fewer keys are
+// not, since the join costs more than it saves.
+constexpr int kCutWaves = 4, kCutKeys = 20 * kTileKeys;
 
-template <int D>
+template <int D, bool PAIR>
 static cudaError_t launch_prefill4(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
-  const int tiles = ceil_div((long long)a.k.c.max_tokens * a.group, 2 * kTileRows);
-  const long long ctas = (long long)tiles * a.k.c.kv_heads * a.k.c.seqs;
-  if (tiles > 65535) return cudaErrorInvalidValue;
-  // Grids that leave half of the SMs without a CTA are split along the keys, but not below
-  // two tiles of 128 keys a CTA.
-  const long long key_tiles = ceil_div(a.window > 0 && a.window + a.sinks < a.k.c.max_len - a.k.c.max_tokens
-                                           ? (long long)a.window + a.sinks + a.k.c.max_tokens
-                                           : a.k.c.max_len,
-                                       kTileKeys);
-  long long nsplit = num_sms / ctas;
-  if (nsplit > key_tiles / 2) nsplit = key_tiles / 2;
-  if constexpr (D == 128) {
-    if (nsplit <= 1 && (long long)a.k.c.max_tokens * a.group >= kPairRows) {
-      const auto pair = kv4_prefill_kernel<D, false, true>;
-      const cudaError_t e = ensure_max_dyn_smem(pair);
-      if (e != cudaSuccess) return e;
-      const int tiles4 = ceil_div((long long)a.k.c.max_tokens * a.group, 4 * kTileRows);
-      return launch_after(pair, dim3(2 * a.k.c.kv_heads, a.k.c.seqs, tiles4), kPreThreads, PreLayout<D, true, (int)sizeof(Pre4Shared)>::kBytes, s, 2,
-                          a, 1);
-    }
+  constexpr int kCtas = PAIR ? 2 : 1, kRows = kCtas * 2 * kTileRows;
+  constexpr int smem = PreLayout<D, PAIR, (int)sizeof(Pre4Shared)>::kBytes;
+  const Kv8Args& c = a.k.c;
+  const long long P = std::max(num_sms / kCtas, 1), each = ceil_div((long long)c.max_tokens * a.group, kRows);
+  // Most tasks that there can be: whole tiles of all rows, and each sequence's last one.
+  const long long tasks = std::min((long long)c.tokens * a.group / kRows + c.seqs, each * c.seqs) * c.kv_heads;
+  // The tasks that would be cut are the last ones, with the fewest keys: those of a call's context, or, where all tasks run
+  // at once, up to all of its keys.  A part has two tiles of 128 keys at least.
+  auto seen = [&](long long keys) { return a.window > 0 ? std::min(keys, (long long)a.window + a.sinks + c.max_tokens) : keys; };
+  const long long keys = seen(tasks < P ? c.max_len : c.max_len - c.max_tokens);
+  if (c.seqs > kFewSeqs || tasks >= kCutWaves * P || 3 * (tasks % P) > 2 * P || keys < kCutKeys) {
+    const auto fn = kv4_prefill_kernel<D, PAIR, false>;
+    const cudaError_t e = ensure_max_dyn_smem(fn);
+    if (e != cudaSuccess) return e;
+    if (each > 65535) return cudaErrorInvalidValue;
+    return launch_after(fn, dim3((unsigned)(kCtas * c.kv_heads), c.seqs, (unsigned)each), kPreThreads, smem, s, kCtas, a, 0, 1);
   }
-  constexpr int smem = PreLayout<D, false, (int)sizeof(Pre4Shared)>::kBytes;
-  const auto fn = nsplit > 1 ? kv4_prefill_kernel<D, true, false> : kv4_prefill_kernel<D, false, false>;
-  const cudaError_t e = ensure_max_dyn_smem(fn);
+  const auto fn = kv4_prefill_kernel<D, PAIR, true>;
+  cudaError_t e = ensure_max_dyn_smem(fn);
   if (e != cudaSuccess) return e;
-  if (nsplit <= 1) return launch_after(fn, dim3(a.k.c.kv_heads, a.k.c.seqs, tiles), kPreThreads, smem, s, 1, a, 1);
-  const cudaError_t e2 =
-      launch_after(fn, dim3(a.k.c.kv_heads, a.k.c.seqs, (unsigned)(tiles * nsplit)), kPreThreads, smem, s, 1, a, (int)nsplit);
-  if (e2 != cudaSuccess) return e2;
-  const int rows = a.k.c.max_tokens * a.group;
-  return launch_after(kv4_join_kernel<D>, dim3(ceil_div(rows, 8), a.k.c.kv_heads, a.k.c.seqs), 256, 0, s, 1, a, (int)nsplit,
-                      tiles);
+  const int most = (int)(keys / (2 * kTileKeys));
+  const long long parts = tasks < P ? std::max(P, std::min(3 * tasks, 2 * P)) : tasks + 4 * P / 3;
+  e = launch_after(fn, dim3((unsigned)(kCtas * parts)), kPreThreads, smem, s, kCtas, a, (int)P, most);
+  if (e != cudaSuccess) return e;
+  return launch_after(kv4_join_kernel<D>, dim3(kRows / (kJoinThreads / 32), (unsigned)std::min(tasks, 2 * P / 3)), kJoinThreads, 0,
+                      s, 1, a, kRows, (int)P, most);
 }
 
 cudaError_t launch_kv4_prefill(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
-  return a.k.c.head_dim == 64 ? launch_prefill4<64>(a, num_sms, s) : launch_prefill4<128>(a, num_sms, s);
+  if (a.k.c.head_dim == 64) return launch_prefill4<64, false>(a, num_sms, s);
+  return (long long)a.k.c.max_tokens * a.group >= kPairRows ? launch_prefill4<128, true>(a, num_sms, s)
+                                                             : launch_prefill4<128, false>(a, num_sms, s);
 }
 
 }  // namespace dptq
