@@ -58,6 +58,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 constexpr int kNG = 4;
+constexpr int kDec4MinSteps = 4, kDec4Join = 20;   // (MIN a power of two)
 constexpr float kDecUnit = 15.f;   // weights are relative to 2^-15 of the largest
 
 template <int D, int RT, int NG>   // RT: tiles of 8 rows (1 or 2)
@@ -86,7 +87,7 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
   pdl_launch_dependents();
   pdl_wait();
 
-  decode_shares<D, R, kKeys>(c, A, S, sm, sizeof(Ring), [&](const Seq& q, int s, const Steps& st, int head, int i0, int i1) {
+  decode_shares<D, R, kKeys, kDec4MinSteps, kDec4Join, true>(c, A, S, sm, sizeof(Ring), [&](const Seq& q, int s, const Steps& st, int head, int i0, int i1) {
     const int rows = q.n * A.group;
     // ---- this share's rows of q, in the order of the dims that a widened word has
     uint32_t qf[RT][D / 16][2];

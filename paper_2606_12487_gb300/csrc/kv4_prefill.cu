@@ -158,9 +158,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
   const int rank = PAIR ? blockIdx.x & 1 : 0;
   pdl_launch_dependents();
   pdl_wait();
-  Cut cut;
+  Cut cut{0, 0, 1};
   Task task;
-  int part;
+  int part = 0;
   const int index = blockIdx.x / kCtas;
   if constexpr (CUT) {
     if (!find_task(c, A.group, kRows, index, P, most, blockIdx.x == 0 && warp == 0, cut, task, part)) return;
@@ -232,8 +232,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
     reg_more<160>();
     const int t = warp >> 2, r = tid & (kTileRows - 1), row = row0 + (t * kCtas + rank) * kTileRows + r;
     const bool mine = row < row0 + nrows;
-    const int tok = row / A.group, hh = row - tok * A.group;
-    const int pos = mine ? q.start + tok : -1;
+    const int pos = mine ? q.start + row / A.group : -1;
     const uint32_t tlane = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tm + tlane + t * 128, tO = tm + tlane + 256 + t * 128;
     float m = -INFINITY, l = 0.f;

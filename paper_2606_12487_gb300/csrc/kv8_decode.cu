@@ -38,6 +38,10 @@
 namespace dptq {
 
 constexpr int kDecKeys = 32;        // keys of a step
+// Fewest steps that a CTA is started for: one a warp (one sequence, 8 heads, with 4 / 8 steps, us: of 512 tokens
+// 9.5 / 10.1, of 2048 12.8 / 10.9, of 8192 13.5 / 16.6).  Most partial results joined at once (57 of one sequence of 131072 tokens in two levels: 54.9 us;
+// in one: 59.3 us).
+constexpr int kDecMinSteps = 4, kDecJoin = 12;
 // Four codes of two keys to four pairs (key a, key b).
 __device__ __forceinline__ void widen_pairs(uint32_t a, uint32_t b, uint32_t (&r)[4]) {
   const uint32_t lo = __byte_perm(a, b, 0x5140) ^ 0x80808080u, hi = __byte_perm(a, b, 0x7362) ^ 0x80808080u;
@@ -75,7 +79,7 @@ kv8_decode_kernel(const Kv8AttendArgs A) {
   pdl_launch_dependents();
   pdl_wait();
 
-  decode_shares<D, R, kDecKeys>(c, A, S, sm, sizeof(Ring<D>), [&](const Seq& q, int s, const Steps& st, int head, int i0, int i1) {
+  decode_shares<D, R, kDecKeys, kDecMinSteps, kDecJoin, false>(c, A, S, sm, sizeof(Ring<D>), [&](const Seq& q, int s, const Steps& st, int head, int i0, int i1) {
     const int rows = q.n * A.group;
 
     // ---- this share's rows of q, in the order of the dims that the keys' bytes have

@@ -14,10 +14,8 @@
 namespace dptq {
 
 constexpr int kDecWarps = 4, kDecThreads = 32 * kDecWarps;
-// Fewest steps that a CTA is started for: one a warp (one sequence, 8 heads, with 4 / 8 steps, us: of 512 tokens
-// 9.5 / 10.1, of 2048 12.8 / 10.9, of 8192 13.5 / 16.6).  Most partial results joined at once (57 of one sequence of 131072 tokens in two levels: 54.9 us;
-// in one: 59.3 us), and of a group, or groups: sqrt of a grid of 1024 CTAs at most.
-constexpr int kDecMinSteps = 4, kDecJoin = 12, kDecJoinMost = 32;
+// Most partial results of a group, or groups: sqrt of a grid of 1024 CTAs at most.
+constexpr int kDecJoinMost = 32;
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
@@ -91,6 +89,7 @@ template <int R>
 struct JoinShared {
   float m[kDecWarps][R], l[kDecWarps][R];
   int red[kDecWarps], found[3];
+  int3 sums[kDecWarps];
   float part_m[kDecJoinMost][R], part_l[kDecJoinMost][R];
   uint32_t arrived;
 };
@@ -98,16 +97,21 @@ struct JoinShared {
 // Runs body(q, s, st, head, i0, i1) for each run of steps i0 .. i1 - 1 of a (sequence s, KV head) in this CTA's share.
 // Every warp leaves its rows' weighted values [R][D] in its own memory (at `mem`, `pitch` bytes apart), and
 // maxima and sums in S; they are joined here, across CTAs too, and written.
-template <int D, int R, int KEYS, class Args, class Body>
+// MIN: fewest steps that a CTA is started for.  JOIN: most partial results joined at once.
+// ALIGN: calls that do not fill the grid are cut by (sequence, head) instead: CTAs of MIN or 2 MIN steps of one head, as long as its
+// results are joined at once.  A head's steps are then counted up to a multiple of that, the ones that are none first.
+template <int D, int R, int KEYS, int MIN, int JOIN, bool ALIGN, class Args, class Body>
 __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, JoinShared<R>& S, const uint8_t* mem,
                                               size_t pitch, Body body) {
   constexpr int kSlot = R * D + 2 * R;   // floats of a partial result
+  static_assert(JOIN <= kDecJoinMost, "results joined at once");
   const int tid = threadIdx.x;
   // ---- this CTA's share
   long long total = 0;
   int some = 0;   // sequences with steps
   bool none = false;   // a sequence of rows without a key
   int mine = 0, ahead = 0;   // this thread's sequence of the last 128: its steps, those before it
+  int most = 0, ctas1 = 0, ctas2 = 0;   // (ALIGN) the most steps of a head, CTAs of MIN and 2 MIN steps for one head of each sequence
   for (int s0 = 0; s0 < c.seqs; s0 += kDecThreads) {
     Seq q;
     int n = 0, all;
@@ -118,13 +122,46 @@ __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, J
     ahead = block_scan(n, S.red, all);
     mine = n;
     total += all;
+    if constexpr (ALIGN) {
+      most = max(most, n);
+      ctas1 += (n + MIN - 1) / MIN;
+      ctas2 += (n + 2 * MIN - 1) / (2 * MIN);
+    }
     some += __syncthreads_count(n > 0);
   }
   total *= c.kv_heads;
-  long long ctas = (total + kDecMinSteps - 1) / kDecMinSteps;
+  long long ctas = (total + MIN - 1) / MIN;
   if (ctas > gridDim.x) ctas = gridDim.x;
   const int extra = total >= (long long)kDecExtraFrom * ctas ? kDecExtra : 0;
-  total += (long long)extra * some * c.kv_heads;
+  int unit = 0;   // steps of a CTA of a call that is cut by heads
+  if constexpr (ALIGN) {
+    // (of up to 128 sequences: their steps are at hand)
+    most = __reduce_max_sync(0xffffffffu, most);
+    ctas1 = __reduce_add_sync(0xffffffffu, ctas1);
+    ctas2 = __reduce_add_sync(0xffffffffu, ctas2);
+    if ((tid & 31) == 0) S.sums[tid >> 5] = make_int3(most, ctas1, ctas2);
+    __syncthreads();
+    most = ctas1 = ctas2 = 0;
+#pragma unroll
+    for (int w = 0; w < kDecWarps; ++w) {
+      most = max(most, S.sums[w].x);
+      ctas1 += S.sums[w].y;
+      ctas2 += S.sums[w].z;
+    }
+    if (c.seqs <= kDecThreads && most > 0) {
+      const bool fit1 = (long long)ctas1 * c.kv_heads <= gridDim.x, fit2 = (long long)ctas2 * c.kv_heads <= gridDim.x;
+      if (fit2 && most <= 2 * MIN) unit = 2 * MIN;        // one CTA a head, nothing to join
+      else if (fit1 && most <= JOIN * MIN) unit = MIN;
+      else if (fit2 && most <= JOIN * 2 * MIN) unit = 2 * MIN;
+      if (unit) ctas = (long long)(unit == MIN ? ctas1 : ctas2) * c.kv_heads;
+    }
+  }
+  // A head's steps as they are cut.
+  auto counted = [&](int n) {
+    if (ALIGN && unit) return (n + unit - 1) & -unit;
+    return n > 0 ? n + extra : 0;
+  };
+  total = ALIGN && unit ? ctas * unit : total + (long long)extra * some * c.kv_heads;
   // (such a sequence has no step: zeros, from CTA 0)
   if (blockIdx.x == 0 && __syncthreads_or(none)) {
     for (int s = 0; s < c.seqs; ++s) {
@@ -146,7 +183,11 @@ __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, J
     }
     __syncthreads();
   };
-  if (c.seqs <= kDecThreads && (extra == 0 || some == c.seqs)) {   // from the sums at hand
+  if (ALIGN && unit) {
+    int all;
+    const int n = counted(mine), at = block_scan(n, S.red, all);
+    find(tid, n, (long long)at * c.kv_heads);
+  } else if (c.seqs <= kDecThreads && (extra == 0 || some == c.seqs)) {   // from the sums at hand
     find(tid, mine > 0 ? mine + extra : 0, ((long long)ahead + (long long)extra * tid) * c.kv_heads);
   } else {
     long long before = 0;
@@ -160,20 +201,20 @@ __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, J
       if (before > begin) break;
     }
   }
-  int s = S.found[0], head = S.found[1], v0 = S.found[2];   // (v: steps with the extra ones)
+  int s = S.found[0], head = S.found[1], v0 = S.found[2];   // (v: steps as they are counted)
 
   Seq q;
   load_seq(c, s, q, false);
   Steps st = seq_steps<KEYS>(q, A.window, A.sinks);
   for (long long it = begin; it < end;) {
-    const int vs = st.count + extra, v1 = (int)(end - it < vs - v0 ? v0 + (end - it) : vs);
-    const int i0 = v0 > extra ? v0 - extra : 0, i1 = v1 - extra;
+    const int vs = counted(st.count), pad = vs - st.count, v1 = (int)(end - it < vs - v0 ? v0 + (end - it) : vs);
+    const int i0 = v0 > pad ? v0 - pad : 0, i1 = v1 - pad;
     if (i1 > i0) {
       const int rows = q.n * A.group;
       body(q, s, st, head, i0, i1);
       __syncthreads();
       const bool whole = i0 == 0 && i1 == st.count;
-      const long long seg0 = it - v0 + extra;   // the (sequence, head)'s steps: seg0 .. seg0 + count - 1
+      const long long seg0 = it - v0 + pad;   // the (sequence, head)'s steps: seg0 .. seg0 + count - 1
       float* slot = A.ws + (size_t)(2 * blockIdx.x + (i0 == 0 ? 1 : 0)) * kSlot;
       for (int k = tid; k < rows * D; k += kDecThreads) {
         const int row = k / D, d = k - row * D;
@@ -262,7 +303,7 @@ __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, J
           }
         };
         int per = n;
-        if (n > kDecJoin) {
+        if (n > JOIN) {
           per = 1;
           while (per * per < n) ++per;
           const int b0 = c0 + ((int)blockIdx.x - c0) / per * per, cnt = c1 - b0 + 1 < per ? c1 - b0 + 1 : per;
@@ -270,8 +311,8 @@ __device__ __forceinline__ void decode_shares(const Kv8Args& c, const Args& A, J
           if (!last_of(A.counters + (b0 == c0 ? 2 : 1) * gridDim.x + b0, cnt)) per = 0;
           if (per) join(b0, 1, cnt, false);
         }
-        if (per && last_of(A.counters + c0, n > kDecJoin ? (n + per - 1) / per : n))
-          join(c0, n > kDecJoin ? per : 1, n > kDecJoin ? (n + per - 1) / per : n, true);
+        if (per && last_of(A.counters + c0, n > JOIN ? (n + per - 1) / per : n))
+          join(c0, n > JOIN ? per : 1, n > JOIN ? (n + per - 1) / per : n, true);
       }
       __syncthreads();
     }
