@@ -1,13 +1,13 @@
 """A small LLaMA-shaped decoder on the library: prompts, then single tokens, for a ragged batch.
 
-    python examples/decoder_layers.py
+    python examples/decoder_layers.py [8 or 4, the bits of the KV cache]
 
 Each layer runs, in order (d the width, random weights):
 
   dptq_add_rmsnorm_quant   residual addition, RMS norm, codes       -> q|k|v (dptq_qgemm_codes)
-  (rotary embedding, plain torch)
-  dptq_kv8_append          the new k and v into the int8 paged cache
-  dptq_kv8_attention       over it, causal, with a window and sinks if asked for
+  dptq_rotary              rotary positions of q and k, in place, scaled for long contexts if asked for
+  dptq_kv8_append          the new k and v into the int8 paged cache (kv_bits = 4: dptq_kv4_append)
+  dptq_kv8_attention       over it, causal, with a window and sinks if asked for (dptq_kv4_attention)
   dptq_qlinear             o, behind the online Hadamard rotation
   dptq_add_rmsnorm_quant                                            -> gate|up (dptq_qgemm_codes)
   (SwiGLU, plain torch)
@@ -30,9 +30,13 @@ EPS = 1e-5
 
 class Decoder:
     def __init__(self, layers=4, d=1024, heads=16, kv_heads=4, f=2816, mask_a8=(0, 1, 3), pages=256, page=16,
-                 had_block=256, window=0, sinks=0, seed=0):
+                 had_block=256, window=0, sinks=0, seed=0, kv_bits=8, rotary=None):
         self.d, self.heads, self.kv, self.dim, self.f = d, heads, kv_heads, d // heads, f
         self.page, self.window, self.sinks = page, window, sinks
+        self.rotary = dptq.Rotary(self.dim, **(rotary or {}))
+        cache = {4: dptq.Kv4Cache, 8: dptq.Kv8Cache}[kv_bits]
+        self.append = {4: dptq.dptq_kv4_append, 8: dptq.dptq_kv8_append}[kv_bits]
+        self.attention = {4: dptq.dptq_kv4_attention, 8: dptq.dptq_kv8_attention}[kv_bits]
         self.bits = [8 if i in mask_a8 else 4 for i in range(layers)]
         g = torch.Generator(device="cuda").manual_seed(seed)
 
@@ -45,7 +49,7 @@ class Decoder:
         n_qkv = (heads + 2 * kv_heads) * self.dim
         self.layers = [dict(qkv=dptq.dptq_pack_weights(w(n_qkv, d), 1), o=dptq.dptq_pack_weights(w(d, d), had_block),
                             up=dptq.dptq_pack_weights(w(2 * f, d), 1), down=dptq.dptq_pack_weights(w(d, f), had_block),
-                            g1=gamma(), g2=gamma(), cache=dptq.Kv8Cache.empty(pages, kv_heads, page, self.dim))
+                            g1=gamma(), g2=gamma(), cache=cache.empty(pages, kv_heads, page, self.dim))
                        for _ in range(layers)]
         self.free = list(range(pages))
         self.tables, self.lens = {}, {}
@@ -63,20 +67,13 @@ class Decoder:
         cols = max(len(self.tables[s]) for s in new)
         table = [self.tables[s] + [-1] * (cols - len(self.tables[s])) for s in new]
         i32 = dict(dtype=torch.int32, device="cuda")
-        pos = torch.cat([torch.arange(self.lens[s] - n, self.lens[s]) for s, n in new.items()])
         return dptq.Kv8Batch(torch.tensor(cu, **i32), torch.tensor(lens, **i32), torch.tensor(table, **i32),
-                             tokens=cu[-1], max_tokens=max(new.values()), max_len=max(lens)), pos.cuda()
-
-    def rotary(self, x, pos):
-        half = self.dim // 2
-        a = pos[:, None, None] * 10000.0 ** (-torch.arange(half, device="cuda") / half)
-        u, v = x[..., :half].float(), x[..., half:].float()
-        x.copy_(torch.cat([u * a.cos() - v * a.sin(), u * a.sin() + v * a.cos()], dim=-1))
+                             tokens=cu[-1], max_tokens=max(new.values()), max_len=max(lens))
 
     def step(self, x, new):
         """Hidden states float16 [tokens, d] of the new tokens of the sequences in `new` (a dict of
         counts) through all layers; returns the residual stream after the last one."""
-        batch, pos = self.batch(new)
+        batch = self.batch(new)
         T, half = x.shape[0], dict(dtype=torch.float16, device="cuda")
         h, update = torch.zeros_like(x), x
         scales, att = torch.empty((T,), device="cuda"), torch.empty((T, self.heads, self.dim), **half)
@@ -89,10 +86,9 @@ class Decoder:
             dptq.dptq_qgemm_codes(layer["qkv"], codes, scales, bits, qkv)
             rows = qkv.unflatten(1, (self.heads + 2 * self.kv, self.dim))
             q, k, v = rows.split([self.heads, self.kv, self.kv], dim=1)
-            self.rotary(q, pos)
-            self.rotary(k, pos)
-            dptq.dptq_kv8_append(layer["cache"], batch, k, v)
-            dptq.dptq_kv8_attention(layer["cache"], batch, q, att, 1 / math.sqrt(self.dim), self.window, self.sinks)
+            dptq.dptq_rotary(self.rotary, batch, rows[:, :self.heads + self.kv])
+            self.append(layer["cache"], batch, k, v)
+            self.attention(layer["cache"], batch, q, att, 1 / math.sqrt(self.dim), self.window, self.sinks)
             dptq.dptq_qlinear(layer["o"], att.flatten(1), bits, proj)
             dptq.dptq_add_rmsnorm_quant(proj, h, layer["g2"], EPS, bits, h, codes, scales)
             dptq.dptq_qgemm_codes(layer["up"], codes, scales, bits, up)
@@ -102,8 +98,8 @@ class Decoder:
         return h + update
 
 
-def main():
-    model = Decoder()
+def main(kv_bits=8):
+    model = Decoder(kv_bits=kv_bits)
     g = torch.Generator(device="cuda").manual_seed(1)
     new = {0: 37, 1: 120, 2: 5}
     y = model.step(torch.randn((sum(new.values()), model.d), generator=g, device="cuda").half(), new)
@@ -122,4 +118,4 @@ def main():
 
 
 if __name__ == "__main__":
-    main()
+    main(kv_bits=int(sys.argv[1]) if len(sys.argv) > 1 else 8)

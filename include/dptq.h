@@ -270,7 +270,9 @@ dptq_status dptq_kv8_reserve(void);
  * dptq_kv4_quantize (two's complement, low nibble = even dim); scales bfloat16 (raw bits)
  * [num_blocks][kv_heads][block_tokens].  Codes and scales 16-byte aligned.  A cached value is
  * binary16(scale * code), which is exact for scales of 2^-17 and more (8 + 3 significant bits): the tensor
- * cores, the read-back and the definition below all see the same values.  head_dim 64 or 128;
+ * cores, the read-back and the definition below all see the same values.  Scales are 0 to 9344, the largest that
+ * dptq_kv4_append makes of finite values; anything else counts as no number in dptq_kv4_attention.  Codes are -7 to 7; what
+ * is stored at positions that no query sees is of no consequence.  head_dim 64 or 128;
  * block_tokens 16, 32, 64 or 128; num_blocks * kv_heads * block_tokens below 2^32 (UNSUPPORTED otherwise).
  * All device memory of the caller; the struct is read during the call only. */
 typedef struct dptq_kv4_cache {
@@ -303,9 +305,10 @@ dptq_status dptq_kv4_read(const dptq_kv4_cache* cache, const dptq_kv8_batch* bat
  * h / (q_heads / kv_heads):
  *   out = sum_j softmax(scale * q . k_j)_j v_j  over the keys j that the query sees,
  * as dptq_kv8_attention defines them (window, sinks, zeros for a query that sees none).  A query that sees a key
- * whose K or V scale is infinite or NaN gets NaN; no other query is touched by it, and NaN in q
- * stays in its row.  Logits, maxima, sums and accumulators are fp32; softmax weights are rounded to binary16
- * relative to their largest so far.
+ * whose K or V scale is no number (negative, above 9344, infinite or NaN) gets NaN; no other query is touched by it, and
+ * NaN in q stays in its row.  Logits, maxima, sums and accumulators are fp32; softmax weights are rounded to binary16
+ * relative to their largest so far.  Calls of at most 16 rows for each sequence and KV head take scale * code unrounded
+ * (scales below 2^-17: up to 2^-25 from the value above).
  * Uses the scratch of dptq_kv8_attention (dptq_kv8_reserve allocates it).  Arguments and errors as there. */
 dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,
                                long long q_stride, int q_heads, float scale, int window, int sinks, void* out_fp16,

@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const Kv4RowsArgs
   for (int i = 0; i < V; ++i) {
     const int row = w.row0 + i * w.step;
     const float s = bf16_float(scale[i]);
-    const uint4 v = kv4_tiny(scale[i]) || kv4_bad(scale[i]) ? values_slow(codes[i], s) : nib.values(codes[i], __float2half2_rn(s));
+    const uint4 v = kv4_odd(scale[i]) || kv4_bad(scale[i]) ? values_slow<false>(codes[i], s) : nib.values(codes[i], __float2half2_rn(s));
     if (row < w.end && from[i] >= 0)   // (from the order 0 4, 1 5, 2 6, 3 7)
       *reinterpret_cast<uint4*>(dst + row * a.stride) =
           make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.x, v.y, 0x7632),

@@ -30,7 +30,7 @@ namespace dptq {
 template <int D, int NG>
 struct alignas(128) Ring4 {
   static constexpr int kKeys = 16 * NG, kHalf = kKeys * D / 2;   // bytes of K (and of V)
-  static constexpr int kStages = (NG == 2 ? 6144 : 8192) / kHalf;
+  static constexpr int kStages = 8192 / kHalf;                   // 16 KB a warp
   uint8_t kv[kStages][2 * kHalf];
   uint16_t scale[kStages][2][kKeys];
   float4 factor[kKeys];      // of a step's keys: x = a S + b; 1 / sv
@@ -349,9 +349,8 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
 
 template <int D, int RT>
 static cudaError_t launch_decode4(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int NG = RT == 1 ? kNG : 2;
-  const auto fn = kv4_decode_kernel<D, RT, NG>;
-  const size_t smem = sizeof(Ring4<D, NG>) * kDecWarps;
+  const auto fn = kv4_decode_kernel<D, RT, kNG>;
+  const size_t smem = sizeof(Ring4<D, kNG>) * kDecWarps;
   const cudaError_t e = ensure_max_dyn_smem(fn);
   if (e != cudaSuccess) return e;
   static_assert(kDecode4Ctas8 * 256 <= kDecJoinMost * kDecJoinMost, "groups of a join");   // (up to 256 SMs)

@@ -34,8 +34,9 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return y;
 }
 
-// Below 2^-17 a scale itself is no binary16 number.
-__device__ __forceinline__ bool kv4_tiny(uint32_t scale_bits) { return scale_bits != 0 && scale_bits < 0x3700u; }
+// Below 2^-17 a scale itself is no binary16 number, and from 8192 on -8 times it is none (a code that append does not make,
+// but that unused memory may hold).
+__device__ __forceinline__ bool kv4_odd(uint32_t scale_bits) { return scale_bits - 1u < 0x36FFu || scale_bits - 0x4600u < 0x100u; }
 
 // The nibbles of a word of eight codes, two a register, in the order 0 4, 1 5, 2 6, 3 7.  A nibble with its sign flipped is
 // code + 8.  With its constants in registers a mask and the flip are one instruction.
@@ -84,9 +85,13 @@ struct Nibbles {
     return make_uint4(v[0], v[1], v[2], v[3]);
   }
 };
-// The values for any scale: each product in fp32, rounded once.
+// The values for any scale: each product in fp32, rounded once.  FINITE: at most the largest number of binary16.
+template <bool FINITE>
 __device__ __forceinline__ uint4 values_slow(uint32_t w, float s) {
-  auto value = [&](int e) { return s * (float)((int)(w << (28 - 4 * e)) >> 28); };
+  auto value = [&](int e) {
+    const float v = s * (float)((int)(w << (28 - 4 * e)) >> 28);
+    return FINITE ? fminf(fmaxf(v, -65504.f), 65504.f) : v;
+  };
   return make_uint4(pack_half2(value(0), value(4)), pack_half2(value(1), value(5)), pack_half2(value(2), value(6)),
                     pack_half2(value(3), value(7)));
 }

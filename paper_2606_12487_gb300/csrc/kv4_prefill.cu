@@ -472,21 +472,21 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
       const bool other = lanes == 4 && col >= 2;
       dst += other ? (kv ? L::kHalf : L::kKHalf) : 0;
       uint32_t sb[kUnits];
-      bool tiny = false;
+      bool odd = false;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
         // A scale that is no number makes its key's K values NaN, so that its scores are for the rows that see it, and its
         // V values 0, so that no other row meets it.
         const bool bad = kv4_bad(max(sk[i], sv[i]));
         sb[i] = kv ? (bad ? 0u : sv[i]) : (bad ? 0x7FC0u : sk[i]);
-        tiny |= kv4_tiny(sb[i]);
+        odd |= kv4_odd(sb[i]);
       }
       const int chunk = 4 * (col & 1) + (other ? 2 : 0);
       auto place = [&](int i, int k) {   // of word k of unit i
         const int at = key_in(i, kv) - (kv ? 0 : rank * (kTileKeys / kCtas));
         return reinterpret_cast<uint4*>(dst + at * 128 + (((chunk ^ k) ^ (at & 7)) << 4));
       };
-      if (!__any_sync(0xffffffffu, tiny)) {
+      if (!__any_sync(0xffffffffu, odd)) {
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
           const uint32_t x[4] = {other ? v[i].z : v[i].x, other ? v[i].w : v[i].y, other ? v[i].x : v[i].z, other ? v[i].y : v[i].w};
@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
 #pragma unroll 1
           for (int k = 0; k < 4; ++k) {
             const int from = other ? k ^ 2 : k;
-            *place(i, k) = values_slow(from == 0 ? v[i].x : from == 1 ? v[i].y : from == 2 ? v[i].z : v[i].w, bf16_float(sb[i]));
+            *place(i, k) = values_slow<true>(from == 0 ? v[i].x : from == 1 ? v[i].y : from == 2 ? v[i].z : v[i].w, bf16_float(sb[i]));
           }
         }
       }
@@ -688,8 +688,14 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(const Kv4AttendA
   for (int e = 0; e < E; e += 2) *reinterpret_cast<__half2*>(dst + e) = __floats2half2_rn(o[e] * inv, o[e + 1] * inv);
 }
 
-// Rows of a sequence and KV head from which pairs of CTAs take them.
-constexpr int kPairRows = 512;
+// Of so many keys of a sequence, those that its rows see.
+static long long keys_seen(const Kv4AttendArgs& a, long long keys) {
+  return a.window > 0 ? std::min(keys, (long long)a.window + a.sinks + a.k.c.max_tokens) : keys;
+}
+// Pairs of CTAs take sequences of so many rows (of a KV head) and, on average over the rows, so many keys.  Pairs / CTAs
+// alone, us, 64 over 8 heads: 1 x 8192 838 / 942; 1 x 512 behind 16000 220 / 259; 1 x 2048 behind 8000 466 / 506; 16 x 100 behind
+// 4000 209 / 208; 1 x 1000 behind 100000 2555 / 3056; with fewer keys 32 heads, 8 x 512 64 / 47; 32 over 8, 3 x 2048 101 / 100.
+constexpr int kPairRows = 512, kPairKeys = 2048;
 // Calls of so many waves are not cut, since their tasks do not end together, and calls whose last tasks have fewer keys are
 // not, since the join costs more than it saves.
 constexpr int kCutWaves = 4, kCutKeys = 20 * kTileKeys;
@@ -704,8 +710,7 @@ static cudaError_t launch_prefill4(const Kv4AttendArgs& a, int num_sms, cudaStre
   const long long tasks = std::min((long long)c.tokens * a.group / kRows + c.seqs, each * c.seqs) * c.kv_heads;
   // The tasks that would be cut are the last ones, with the fewest keys: those of a call's context, or, where all tasks run
   // at once, up to all of its keys.  A part has two tiles of 128 keys at least.
-  auto seen = [&](long long keys) { return a.window > 0 ? std::min(keys, (long long)a.window + a.sinks + c.max_tokens) : keys; };
-  const long long keys = seen(tasks < P ? c.max_len : c.max_len - c.max_tokens);
+  const long long keys = keys_seen(a, tasks < P ? c.max_len : c.max_len - c.max_tokens);
   if (c.seqs > kFewSeqs || tasks >= kCutWaves * P || 3 * (tasks % P) > 2 * P || keys < kCutKeys) {
     const auto fn = kv4_prefill_kernel<D, PAIR, false>;
     const cudaError_t e = ensure_max_dyn_smem(fn);
@@ -726,8 +731,8 @@ static cudaError_t launch_prefill4(const Kv4AttendArgs& a, int num_sms, cudaStre
 
 cudaError_t launch_kv4_prefill(const Kv4AttendArgs& a, int num_sms, cudaStream_t s) {
   if (a.k.c.head_dim == 64) return launch_prefill4<64, false>(a, num_sms, s);
-  return (long long)a.k.c.max_tokens * a.group >= kPairRows ? launch_prefill4<128, true>(a, num_sms, s)
-                                                             : launch_prefill4<128, false>(a, num_sms, s);
+  const bool pairs = (long long)a.k.c.max_tokens * a.group >= kPairRows && keys_seen(a, a.k.c.max_len - a.k.c.max_tokens / 2) >= kPairKeys;
+  return pairs ? launch_prefill4<128, true>(a, num_sms, s) : launch_prefill4<128, false>(a, num_sms, s);
 }
 
 }  // namespace dptq

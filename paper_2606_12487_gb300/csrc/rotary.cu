@@ -130,31 +130,40 @@ __global__ void __launch_bounds__(kRotThreads) rotary_units_kernel(const RotaryA
   }
 }
 
-// Any even rot: a thread a pair, or a value of the rest of a head.
+// Any even rot: pairs cross 16-byte vectors in any way, so a CTA takes a part of a row through shared memory, whole vectors in and
+// out, a thread a pair in between.  (A thread a pair from and to global memory: 8192 rows of 72 heads, rot 20: 162 us.)
+constexpr int kPairValues = 4096;   // values of a part: whole heads
 __global__ void __launch_bounds__(kRotThreads) rotary_pairs_kernel(const RotaryArgs a) {
   __shared__ float cs[kRotMost], sn[kRotMost];
+  __shared__ __align__(16) __half row_s[kPairValues];
   pdl_launch_dependents();
   pdl_wait();
   Seq q;
-  if (!load_seq(a.c, blockIdx.y, q, threadIdx.x == 0 && blockIdx.x == 0)) return;
+  if (!load_seq(a.c, blockIdx.y, q, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.z == 0)) return;
   const int row = max(-q.start, 0) + blockIdx.x;
   if (row >= q.n) return;
+  const int per = kPairValues / a.head_dim, h0 = blockIdx.z * per, heads = min(per, a.heads - h0);
+  const __half* x = a.x + (size_t)(q.tok0 + row) * a.x_stride + (size_t)h0 * a.head_dim;
+  __half* y = a.out + (size_t)(q.tok0 + row) * a.out_stride + (size_t)h0 * a.head_dim;
+  // vectors of a head that change or are copied, of its head_dim / 8
+  const int all = a.head_dim / 8, vecs = a.x == a.out ? (a.rot + 7) / 8 : all, half = a.rot / 2;
+  for (int i = threadIdx.x; i < heads * vecs; i += kRotThreads) {
+    const int h = i / vecs, v = h * all + i - h * vecs;
+    reinterpret_cast<uint4*>(row_s)[v] = ld_plain(reinterpret_cast<const uint4*>(x) + v);
+  }
   make_angles(a, q.start + row, 1, cs, sn);
   __syncthreads();
-  const __half* x = a.x + (size_t)(q.tok0 + row) * a.x_stride;
-  __half* y = a.out + (size_t)(q.tok0 + row) * a.out_stride;
-  const int half = a.rot / 2, items = half + (a.x == a.out ? 0 : a.head_dim - a.rot);
-  for (int i = threadIdx.x; i < a.heads * items; i += kRotThreads) {
-    const int h = i / items, k = i - h * items, d = h * a.head_dim;
-    if (k >= half) {
-      y[d + half + k] = ld_plain(x + d + half + k);
-      continue;
-    }
-    const int d0 = d + (a.interleaved ? 2 * k : k), d1 = d0 + (a.interleaved ? 1 : half);
-    float u = __half2float(ld_plain(x + d0)), v = __half2float(ld_plain(x + d1));
+  for (int i = threadIdx.x; i < heads * half; i += kRotThreads) {
+    const int h = i / half, k = i - h * half, d0 = h * a.head_dim + (a.interleaved ? 2 * k : k), d1 = d0 + (a.interleaved ? 1 : half);
+    float u = __half2float(row_s[d0]), v = __half2float(row_s[d1]);
     turn_pair(u, v, cs[k], sn[k]);
-    y[d0] = __float2half_rn(u);
-    y[d1] = __float2half_rn(v);
+    row_s[d0] = __float2half_rn(u);
+    row_s[d1] = __float2half_rn(v);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < heads * vecs; i += kRotThreads) {
+    const int h = i / vecs, v = h * all + i - h * vecs;
+    reinterpret_cast<uint4*>(y)[v] = reinterpret_cast<const uint4*>(row_s)[v];
   }
 }
 
@@ -167,7 +176,8 @@ static cudaError_t launch_units(const RotaryArgs& a, int parts, cudaStream_t s) 
 cudaError_t launch_rotary(const RotaryArgs& a, int num_sms, cudaStream_t s) {
   const long long rows = (long long)a.c.max_tokens * a.c.seqs;   // (most of them)
   if (a.rot % 16 != 0 || a.head_dim % 16 != 0)
-    return launch_after(rotary_pairs_kernel, dim3(a.c.max_tokens, a.c.seqs), kRotThreads, 0, s, 1, a);
+    return launch_after(rotary_pairs_kernel, dim3(a.c.max_tokens, a.c.seqs, ceil_div(a.heads, kPairValues / a.head_dim)),
+                        kRotThreads, 0, s, 1, a);
   if (a.c.max_tokens >= kRotRows && rows >= (long long)kRotRows * kRotFull * num_sms) return launch_units<kRotRows>(a, 1, s);
   // Few rows: their heads over as many CTAs as there are SMs, while a thread has more than it asks for ahead.
   long long parts = ceil_div((long long)a.heads * (a.head_dim / 16), kAhead * kRotThreads);

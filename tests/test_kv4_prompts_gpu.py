@@ -153,3 +153,20 @@ def test_two_streams_in_turn_share_the_scratch(dp):  # noqa: F811
             dp.dptq_kv4_attention(c, b, q, out, 0.1)
     torch.cuda.synchronize()
     assert all(torch.equal(a, d[3]) for a, d in zip(first, data))
+
+
+@pytest.mark.parametrize("n", [1, 60, 600])
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_largest_values_where_no_query_looks(dp, n, D):  # noqa: F811
+    """Unused memory may hold the code -8, which append does not make: times 9344 it is no binary16 number."""
+    rng = np.random.default_rng(n)
+    cu, lens, table, blocks = ref.random_batch(rng, [n], [200 + n], 16)
+    cache = ref.random_cache(rng, blocks, 1, 16, D)
+    q = _rows(rng, n, 2, D)
+    got, _ = _attend(dp, cache, q, cu, lens, table, window=50)
+    last, used = table[0, (lens[0] - 1) // 16], (lens[0] - 1) % 16 + 1
+    for page, slots in ((last, slice(used, 16)), (table[0, 2], slice(0, 16))):
+        for kv in (0, 2):
+            cache[kv][page, :, slots], cache[kv + 1][page, :, slots] = 0x88, 0x4612
+    again, _ = _attend(dp, cache, q, cu, lens, table, window=50)
+    assert np.array_equal(got, again)
