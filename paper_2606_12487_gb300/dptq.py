@@ -376,18 +376,35 @@ class Kv8Batch:
         self._ref = ctypes.addressof(self._c)
 
 
-def _check_device(*devices):
-    """A call's tensors lie on the current device, whose stream it is launched on."""
+def _launch_stream(stream, *devices) -> int:
+    """The raw stream of a call whose tensors lie on `devices`, which have to be the current one."""
     import torch
-    now = torch.cuda.current_device()
+    now = torch._C._cuda_getDevice()
     for d in devices:
         if d != now:
             raise ValueError(f"tensors must be on the current device ({now}), got one on {d}")
+    return torch._C._cuda_getCurrentRawStream(now) if stream is None else stream.cuda_stream
+
+
+_HALF = None      # torch.float16, once torch is there
 
 
 def _check_heads(t, tokens, heads, dim, name):
     """float16 [tokens, heads, dim] with the heads of a token side by side; tokens any distance apart."""
+    try:   # (one pass over the attributes, as in _check_tensor)
+        if t.dtype is _HALF and t.is_cuda and t.shape == (tokens, heads, dim):
+            st = t.stride()
+            if st[2] == 1 and (st[1] == dim or heads <= 1):
+                return st[0] if tokens > 1 else heads * dim
+    except AttributeError:
+        pass
+    return _check_heads_slowly(t, tokens, heads, dim, name)
+
+
+def _check_heads_slowly(t, tokens, heads, dim, name):
+    global _HALF
     import torch
+    _HALF = torch.float16
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.float16 or not t.is_cuda:
         raise TypeError(f"{name} must be a float16 CUDA tensor")
     if t.shape != (tokens, heads, dim):
@@ -434,6 +451,7 @@ class Kv4Cache:
         _check_tensor(k_scales, torch.bfloat16, (n, h, b), "k_scales")
         _check_tensor(v_scales, torch.bfloat16, (n, h, b), "v_scales")
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        load()
         self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim = n, h, b, 2 * d
         self.device = k_codes.get_device()
         if any(t.get_device() != self.device for t in (v_codes, k_scales, v_scales)):
@@ -456,8 +474,8 @@ def dptq_kv4_append(cache: Kv4Cache, batch: Kv8Batch, k, v, stream=None):
     s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
     if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
         raise ValueError("k and v must have the same distance between tokens")
-    _check_device(cache.device, batch.device, k.get_device(), v.get_device())
-    _check(load().dptq_kv4_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+    at = _launch_stream(stream, cache.device, batch.device, k.get_device(), v.get_device())
+    _check(_lib.dptq_kv4_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, at))
 
 
 def dptq_kv4_read(cache: Kv4Cache, batch: Kv8Batch, k, v, stream=None):
@@ -466,8 +484,8 @@ def dptq_kv4_read(cache: Kv4Cache, batch: Kv8Batch, k, v, stream=None):
     s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
     if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
         raise ValueError("k and v must have the same distance between tokens")
-    _check_device(cache.device, batch.device, k.get_device(), v.get_device())
-    _check(load().dptq_kv4_read(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+    at = _launch_stream(stream, cache.device, batch.device, k.get_device(), v.get_device())
+    _check(_lib.dptq_kv4_read(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, at))
 
 
 def dptq_kv4_attention(cache: Kv4Cache, batch: Kv8Batch, q, out, scale: float, window: int = 0, sinks: int = 0,
@@ -476,9 +494,9 @@ def dptq_kv4_attention(cache: Kv4Cache, batch: Kv8Batch, q, out, scale: float, w
     H = q.shape[1]
     qs = _check_heads(q, batch.tokens, H, cache.head_dim, "q")
     os_ = _check_heads(out, batch.tokens, H, cache.head_dim, "out")
-    _check_device(cache.device, batch.device, q.get_device(), out.get_device())
-    _check(load().dptq_kv4_attention(cache._ref, batch._ref, q.data_ptr(), qs, H, scale, window, sinks,
-                                     out.data_ptr(), os_, _stream(stream)))
+    at = _launch_stream(stream, cache.device, batch.device, q.get_device(), out.get_device())
+    _check(_lib.dptq_kv4_attention(cache._ref, batch._ref, q.data_ptr(), qs, H, scale, window, sinks, out.data_ptr(),
+                                   os_, at))
 
 
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "wavelength": 3, "ramp": 4}
@@ -530,6 +548,7 @@ class Rotary:
         self.frequencies = np.asarray(frequencies, dtype=np.float64)
         self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
         self.device = self.turns.get_device()
+        self.table = self.turns.data_ptr()
 
 
 def dptq_rotary(rotary: Rotary, batch: Kv8Batch, x, out=None, stream=None):
@@ -542,9 +561,9 @@ def dptq_rotary(rotary: Rotary, batch: Kv8Batch, x, out=None, stream=None):
         out = x
     else:
         os_ = _check_heads(out, batch.tokens, H, D, "out")
-    _check_device(rotary.device, batch.device, x.get_device(), out.get_device())
-    _check(load().dptq_rotary(batch._ref, x.data_ptr(), xs, H, D, rotary.turns.data_ptr(), rotary.rot_dim,
-                              rotary.interleaved, rotary.amplitude, out.data_ptr(), os_, _stream(stream)))
+    at = _launch_stream(stream, rotary.device, batch.device, x.get_device(), out.get_device())
+    _check(_lib.dptq_rotary(batch._ref, x.data_ptr(), xs, H, D, rotary.table, rotary.rot_dim, rotary.interleaved,
+                            rotary.amplitude, out.data_ptr(), os_, at))
 
 
 def dptq_kv8_reserve():

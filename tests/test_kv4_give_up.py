@@ -76,7 +76,7 @@ def right(out, want_tol):
     return bool((np.abs(out - want_tol[0]) <= want_tol[1]).all())
 # alone, heads of 64; alone; cut along the keys; pairs; pairs cut along the keys
 for ns, lens, H, g, D in (([300], [900], 80, 2, 64), ([130] * 20, [500] * 20, 8, 1, 128), ([200], [3000], 2, 1, 128),
-                          ([600, 520], [2000, 520], 16, 2, 128), ([600], [3500], 2, 1, 128)):
+                          ([600], [2700], 20, 2, 128), ([600], [3500], 2, 1, 128)):
     call(ns, lens, H, g, D)
     try:
         dptq.dptq_last_device_error()
