@@ -288,8 +288,8 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
         // the half made again.
         float xa[32], xb[32];
         uint32_t p[32];
-        // A quarter's weights, packed, their sum, and its largest score.
-        auto quarter = [&](float (&x)[32], uint32_t* w, float& s, float& top) {
+        // A quarter's weights, packed, and their sum.
+        auto quarter = [&](float (&x)[32], uint32_t* w, float& s) {
           const float off = kUnit - (m == -INFINITY ? 0.f : m);
           const uint64_t a = f2_pack(unit, unit), b = f2_pack(off, off);
           uint64_t sum = 0;
@@ -305,11 +305,13 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
           float s0, s1;
           f2_unpack(sum, s0, s1);
           s += s0 + s1;
+        };
+        auto largest = [&](float (&x)[32]) {
           float v[11];
 #pragma unroll
           for (int k = 0; k < 10; ++k) v[k] = max3(x[3 * k], x[3 * k + 1], x[3 * k + 2]);
           v[10] = fmaxf(x[30], x[31]);
-          top = max3(top, max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8])), fmaxf(v[9], v[10]));
+          return fmaxf(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8])), fmaxf(v[9], v[10]));
         };
         if (j == 0) {   // the first maximum, so that the first half is not made for nothing
 #pragma unroll 1
@@ -327,18 +329,24 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
 #pragma unroll 1
         for (;;) {   // (once, but for maxima that grow: that code stands apart from what every tile runs)
           float top;
+          bool more;
 #pragma unroll 1
           for (; n < 2; ++n) {
             const int h = 2 - 2 * n;
             float s = 0.f;
-            top = -INFINITY;
+            more = false;
             tmem_ld_arrived(xa);
             tmem_ld32(tS + 32 * h + 32, xb);   // (under the first quarter's work)
-            quarter(xa, p, s, top);
+            quarter(xa, p, s);
             tmem_ld_arrived(xb);
-            quarter(xb, p + 16, s, top);
-            top *= unit;
-            if (__any_sync(0xffffffffu, top > m + 8.f)) break;
+            quarter(xb, p + 16, s);
+            // The sum says whether a weight may be above 2^15: the scores' maximum is looked for only then, and where no
+            // key has been seen yet.
+            if (__any_sync(0xffffffffu, s > 32768.f || m == -INFINITY)) {
+              top = unit * fmaxf(largest(xa), largest(xb));
+              more = s > 32768.f || (m == -INFINITY && top > m);
+              if (__any_sync(0xffffffffu, more)) break;
+            }
             l += s;
             tmem_st32(tS + 64 + 32 * n, p);
             if (n == 0) tmem_ld32(tS, xa);
@@ -348,7 +356,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
           }
           if (n == 2) break;
           // (a row whose own maximum may still lag keeps it: its result has nothing to do with the warp's other rows)
-          const float mn = top > m + 8.f ? top : m, f = mn == m ? 1.f : exp2_fast(m - mn);   // (m = -inf: no key yet)
+          const float mn = more ? top : m, f = mn == m ? 1.f : exp2_fast(m - mn);   // (m = -inf: no key yet)
           m = mn;
           l *= f;
           // O: PV of tile j - 1 came before S of tile j, which is here; of tile j, the first half's
