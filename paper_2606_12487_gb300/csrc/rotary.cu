@@ -24,7 +24,7 @@ constexpr int kRotThreads = 256, kRotMost = 256;   // most pairs of a head
 // cos and sin of the pairs of `rows` rows from position `pos` on.
 __device__ __forceinline__ void make_angles(const RotaryArgs& a, int pos, int rows, float* cs, float* sn) {
   const int half = a.rot / 2;
-  for (int i = threadIdx.x; i < rows * half; i += kRotThreads) {
+  for (int i = threadIdx.x; i < rows * half; i += blockDim.x) {
     const int r = i / half, k = i - r * half;
     const uint64_t turn = (uint64_t)(pos + r) * ld_plain(a.turns + k);   // (modulo whole turns)
     float c, s;
@@ -135,9 +135,10 @@ __global__ void __launch_bounds__(kRotThreads) rotary_units_kernel(const RotaryA
 }
 
 // Any even rot: pairs cross 16-byte vectors in any way, so a CTA takes a part of a row through shared memory, whole vectors in and
-// out, a thread a pair in between: 8192 rows of 72 heads, 20 of 128 values, 73 us (a thread a pair from and to global memory: 162).
-constexpr int kPairValues = 4096;   // values of a part: whole heads
-__global__ void __launch_bounds__(kRotThreads) rotary_pairs_kernel(const RotaryArgs a) {
+// out, a thread a pair in between: 8192 rows of 72 heads, 20 of 128 values, 60 us (with 256 threads a part 73, 64 and half a
+// part 63; a thread a pair from and to global memory 162).
+constexpr int kPairThreads = 128, kPairValues = 4096;   // values of a part: whole heads
+__global__ void __launch_bounds__(kPairThreads) rotary_pairs_kernel(const RotaryArgs a) {
   __shared__ float cs[kRotMost], sn[kRotMost];
   __shared__ __align__(16) __half row_s[kPairValues];
   pdl_launch_dependents();
@@ -151,13 +152,13 @@ __global__ void __launch_bounds__(kRotThreads) rotary_pairs_kernel(const RotaryA
   __half* y = a.out + (size_t)(q.tok0 + row) * a.out_stride + (size_t)h0 * a.head_dim;
   // vectors of a head that change or are copied, of its head_dim / 8
   const int all = a.head_dim / 8, vecs = a.x == a.out ? (a.rot + 7) / 8 : all, half = a.rot / 2;
-  for (int i = threadIdx.x; i < heads * vecs; i += kRotThreads) {
+  for (int i = threadIdx.x; i < heads * vecs; i += kPairThreads) {
     const int h = i / vecs, v = h * all + i - h * vecs;
     reinterpret_cast<uint4*>(row_s)[v] = ld_plain(reinterpret_cast<const uint4*>(x) + v);
   }
   make_angles(a, q.start + row, 1, cs, sn);
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * half; i += kRotThreads) {
+  for (int i = threadIdx.x; i < heads * half; i += kPairThreads) {
     const int h = i / half, k = i - h * half, d0 = h * a.head_dim + (a.interleaved ? 2 * k : k), d1 = d0 + (a.interleaved ? 1 : half);
     float u = __half2float(row_s[d0]), v = __half2float(row_s[d1]);
     turn_pair(u, v, cs[k], sn[k]);
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kRotThreads) rotary_pairs_kernel(const RotaryA
     row_s[d1] = __float2half_rn(v);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * vecs; i += kRotThreads) {
+  for (int i = threadIdx.x; i < heads * vecs; i += kPairThreads) {
     const int h = i / vecs, v = h * all + i - h * vecs;
     reinterpret_cast<uint4*>(y)[v] = reinterpret_cast<const uint4*>(row_s)[v];
   }
@@ -181,7 +182,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, int num_sms, cudaStream_t s) {
   const long long rows = (long long)a.c.max_tokens * a.c.seqs;   // (most of them)
   if (a.rot % 16 != 0 || a.head_dim % 16 != 0)
     return launch_after(rotary_pairs_kernel, dim3(a.c.max_tokens, a.c.seqs, ceil_div(a.heads, kPairValues / a.head_dim)),
-                        kRotThreads, 0, s, 1, a);
+                        kPairThreads, 0, s, 1, a);
   if (a.c.max_tokens >= kRotRows && rows >= (long long)kRotRows * kRotFull * num_sms) return launch_units<kRotRows>(a, 1, s);
   // Few rows: their heads over as many CTAs as there are SMs, while a thread has more than it asks for ahead (one row of 640 heads:
   // 2.4 us, in one CTA 5.9; of 80: 2.2 and 2.5).
