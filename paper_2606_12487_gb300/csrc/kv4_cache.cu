@@ -10,9 +10,9 @@
 // binary16, 4-byte words of codes.  Bytes bound both for prompts, the launch for single tokens.  A thread keeps its place
 // in a token (K or V, head, 8 values) and takes V tokens one after the other, all of them asked for before the first is
 // used.
-// Four prompts up to 2048 tokens, 8 heads of 128 (27.6 MB): append 11.0, read 9.0 us in a graph (floor 4.1: lengths, table and rows are three
+// Four prompts up to 2048 tokens, 8 heads of 128 (27.6 MB): append 10.6, read 8.7 us in a graph (floor 4.1: lengths, table and rows are three
 // latencies in a row); a token of each of 32 sequences, 32 heads: 2.4 and 2.7 us.  Read of 32 sequences up to 4096 tokens, 32 heads (1.45
-// GB): 238 us, 6.1 TB/s.
+// GB): 244 us, 5.9 TB/s.
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -23,9 +23,9 @@
 namespace dptq {
 
 constexpr int kRowThreads = 256;
-// Tokens of a thread, of prompts: append of the four 11.4 / 11.0 / 12.2 us with 2 / 4 / 8; read of them 9.9 / 9.0 / 9.4, of the 32
-// sequences 352 / 261 / 244.
-constexpr int kAppendTokens = 4, kReadTokens = 8;
+// Tokens of a thread, of prompts: append of the four 12.9 / 10.6 / 11.7 / 11.7 us with 1 / 2 / 4 / 8; read with 4 / 8 / 16 of them 8.7 / 9.3 /
+// 9.4, of three sequences up to 1500 tokens, 8 heads 6.5 / 6.5 / 7.8, of the 32 sequences 244 / 244 / 237.
+constexpr int kAppendTokens = 2, kReadTokens = 4;
 
 // What a thread works on: place `at` of a row of a head, K or V, and its tokens row0 + i step, i < V, of the sequence's
 // rows (rows past the last one are not there).
@@ -48,21 +48,25 @@ __device__ __forceinline__ bool work_of(const Kv8Args& c, const Seq& q, Work& w)
   w.end = q.n;
   return item < items && t < side && w.row0 < w.end;
 }
-// Where the rows of codes (and the scales) of its tokens stand, in rows of the cache; -1: no such page.
+// Where the rows of codes (and the scales) of its tokens stand, in rows of the cache (fewer than 2^32, checked on the host);
+// returns the tokens that are there and have a page, a bit each (the others' row is one that is there).
 template <int V>
-__device__ __forceinline__ void cache_rows(const Kv8Args& c, const Seq& q, const Work& w, long long (&to)[V]) {
+__device__ __forceinline__ uint32_t cache_rows(const Kv8Args& c, const Seq& q, const Work& w, uint32_t (&to)[V]) {
+  const int* table = c.table + (long long)blockIdx.y * c.table_stride;
+  const int p0 = q.start + w.row0, last = q.start + w.end - 1;
   int entry[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i)   // (all asked for before the first is looked at)
-    entry[i] = ld_plain(c.table + (long long)blockIdx.y * c.table_stride +
-                        ((q.start + min(w.row0 + i * w.step, w.end - 1)) >> c.log2_page));
+  for (int i = 0; i < V; ++i) entry[i] = ld_plain(table + (min(p0 + i * w.step, last) >> c.log2_page));   // (all before the first is looked at)
+  uint32_t held = 0;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int p = q.start + min(w.row0 + i * w.step, w.end - 1);
-    const bool held = entry[i] >= 0 && entry[i] < c.num_blocks;
-    if (!held) atomicCAS(c.bad, 0, kDevBadPage);
-    to[i] = held ? ((((long long)entry[i] * c.kv_heads + w.head) << c.log2_page) + (p & ((1 << c.log2_page) - 1))) : -1;
+    const int p = p0 + i * w.step;
+    const bool ok = (unsigned)entry[i] < (unsigned)c.num_blocks;
+    if (!ok) atomicCAS(c.bad, 0, kDevBadPage);
+    if (ok && p <= last) held |= 1u << i;
+    to[i] = ok ? (((unsigned)entry[i] * c.kv_heads + w.head) << c.log2_page) + (min(p, last) & ((1 << c.log2_page) - 1)) : 0u;
   }
+  return held;
 }
 
 // Eight codes rint(x / s) of a row, a nibble each; r = 1 / s within a unit in its last place.
@@ -71,13 +75,13 @@ __device__ __forceinline__ void cache_rows(const Kv8Args& c, const Seq& q, const
 // or, where a + 1 < b, by 2^(a - b) / S, and 2^(a - b) > 0.4 S / X next to a tie: by more than 0.4 / X > 2^-12.4.  x r is
 // within 2^-19 of the quotient, which is 7.03 at most.  So x r rounded to a multiple of 2^-13 is the tie itself where there
 // is one and on the quotient's side of it elsewhere, and rint of that is rint of the quotient.  (With a check for near ties and a
-// division behind it, two of three warps divided, and the append of four prompts took 16 us in a graph, not 11.)
-__device__ __forceinline__ uint32_t quant8_nibbles(const uint4& v, float s, float r) {
+// division behind it, two of three warps divided, and the append of four prompts took 16 us in a graph instead of 11.)
+// nan: one of the values is.
+__device__ __forceinline__ uint32_t quant8_nibbles(const uint4& v, float s, float r, bool nan) {
   constexpr float kGrid = 1536.f, kMagic = 12582912.f;   // 1.5 2^10 and 1.5 2^23, where fp32 has steps of 2^-13 and 1
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t t[8];
   const uint64_t r2 = f2_pack(r, r), grid = f2_pack(kGrid, kGrid), magic = f2_pack(kMagic, kMagic);
-  bool number = isfinite(s);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[e]));
@@ -89,11 +93,7 @@ __device__ __forceinline__ uint32_t quant8_nibbles(const uint4& v, float s, floa
   const uint32_t even = __byte_perm(__byte_perm(t[0], t[2], 0x0040), __byte_perm(t[4], t[6], 0x0040), 0x5410);
   const uint32_t odd = __byte_perm(__byte_perm(t[1], t[3], 0x0040), __byte_perm(t[5], t[7], 0x0040), 0x5410);
   uint32_t codes = (even & 0x0F0F0F0Fu) | ((odd << 4) & 0xF0F0F0F0u);
-  __half2 am = __habs2(*reinterpret_cast<const __half2*>(&w[0]));
-#pragma unroll
-  for (int e = 1; e < 4; ++e) am = __hmax2_nan(am, __habs2(*reinterpret_cast<const __half2*>(&w[e])));
-  if (!(__hmax_nan(__low2half(am), __high2half(am)) < __ushort_as_half(0x7C00))) number = false;
-  if (!number) {   // NaN takes the code 0, and so does a row with an infinite value
+  if (nan || !isfinite(s)) {   // NaN takes the code 0, and so does a row with an infinite value
     for (int e = 0; e < 8; ++e) {
       const uint32_t h = (w[e >> 1] >> (16 * (e & 1))) & 0x7FFFu;
       if (!isfinite(s) || h > 0x7C00u) codes &= ~(15u << (4 * e));
@@ -113,28 +113,43 @@ __global__ void __launch_bounds__(kRowThreads) kv4_append_kernel(const Kv4RowsAr
   const bool on = work_of<D, V>(c, q, w);
   const unsigned lanes = __ballot_sync(0xffffffffu, on);
   if (!on) return;
-  const __half* src = (w.kv ? a.rows[1] : a.rows[0]) + (long long)q.tok0 * a.stride + w.head * D + 8 * w.at;
+  const __half* src = (w.kv ? a.rows[1] : a.rows[0]) + (q.tok0 + w.row0) * a.stride + (w.head * D + 8 * w.at);
+  const long long step = w.step * a.stride;
   uint4 x[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i)   // (past the last row it once more: a load in a branch would wait for its own data)
-    x[i] = ld_plain(reinterpret_cast<const uint4*>(src + min(w.row0 + i * w.step, w.end - 1) * a.stride));
-  long long to[V];
-  cache_rows(c, q, w, to);
+  for (int i = 0; i < V; ++i) {   // (past the last row it once more: a load in a branch would wait for its own data)
+    x[i] = ld_plain(reinterpret_cast<const uint4*>(src));
+    if (w.row0 + (i + 1) * w.step < w.end) src += step;
+  }
+  uint32_t to[V], nan = 0;
+  const uint32_t held = cache_rows(c, q, w, to);
   float m[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) m[i] = widest(abs_max8(x[i], __half2half2(__ushort_as_half(0))));
+  for (int i = 0; i < V; ++i) {
+    const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    __half2 am = __habs2(*reinterpret_cast<const __half2*>(&v[0]));
+#pragma unroll
+    for (int e = 1; e < 4; ++e) am = __hmax2_nan(am, __habs2(*reinterpret_cast<const __half2*>(&v[e])));
+    m[i] = widest(am);
+    if (__hisnan(__hmax_nan(__low2half(am), __high2half(am)))) {   // it counts for nothing in the maximum
+      nan |= 1u << i;
+      m[i] = widest(abs_max8(x[i], __half2half2(__ushort_as_half(0))));
+    }
+  }
 #pragma unroll
   for (int o = D / 16; o > 0; o >>= 1)
 #pragma unroll
     for (int i = 0; i < V; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(lanes, m[i], o));
+  uint8_t* codes = (w.kv ? a.k.codes[1] : a.k.codes[0]) + 4 * w.at;
+  uint16_t* scales = w.kv ? a.k.scales[1] : a.k.scales[0];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const __nv_bfloat16 sb = __float2bfloat16_rn(__fmul_rn(m[i], 1.f / 7.f));
     const float s = __bfloat162float(sb);
-    const uint32_t codes = quant8_nibbles(x[i], s, s > 0.f ? rcp_fast(s) : 0.f);
-    if (w.row0 + i * w.step < w.end && to[i] >= 0) {
-      *reinterpret_cast<uint32_t*>((w.kv ? a.k.codes[1] : a.k.codes[0]) + to[i] * (D / 2) + 4 * w.at) = codes;
-      if (w.at == 0) (w.kv ? a.k.scales[1] : a.k.scales[0])[to[i]] = __bfloat16_as_ushort(sb);
+    const uint32_t eight = quant8_nibbles(x[i], s, s > 0.f ? rcp_fast(s) : 0.f, nan >> i & 1u);
+    if (held >> i & 1u) {
+      *reinterpret_cast<uint32_t*>(codes + (unsigned long long)to[i] * (D / 2)) = eight;
+      if (w.at == 0) scales[to[i]] = __bfloat16_as_ushort(sb);
     }
   }
 }
@@ -148,8 +163,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const Kv4RowsArgs
   if (!load_seq(c, blockIdx.y, q, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.z == 0)) return;
   Work w;
   if (!work_of<D, V>(c, q, w)) return;
-  long long from[V];
-  cache_rows(c, q, w, from);
+  uint32_t from[V];
+  const uint32_t held = cache_rows(c, q, w, from);
   const uint8_t* src = (w.kv ? a.k.codes[1] : a.k.codes[0]) + 4 * w.at;
   const uint16_t* scales = w.kv ? a.k.scales[1] : a.k.scales[0];
   const Nibbles nib;
@@ -157,18 +172,17 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const Kv4RowsArgs
   uint16_t scale[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const long long at = from[i] < 0 ? 0 : from[i];   // (a row that is there; nothing is written from it)
-    codes[i] = ld_plain(reinterpret_cast<const uint32_t*>(src + at * (D / 2)));
-    scale[i] = ld_plain(scales + at);
+    codes[i] = ld_plain(reinterpret_cast<const uint32_t*>(src + (unsigned long long)from[i] * (D / 2)));
+    scale[i] = ld_plain(scales + from[i]);
   }
-  __half* dst = (w.kv ? a.rows[1] : a.rows[0]) + (long long)q.tok0 * a.stride + w.head * D + 8 * w.at;
+  __half* dst = (w.kv ? a.rows[1] : a.rows[0]) + (q.tok0 + w.row0) * a.stride + (w.head * D + 8 * w.at);
+  const long long step = w.step * a.stride;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int row = w.row0 + i * w.step;
     const float s = bf16_float(scale[i]);
     const uint4 v = kv4_odd(scale[i]) || kv4_bad(scale[i]) ? values_slow<false>(codes[i], s) : nib.values(codes[i], __float2half2_rn(s));
-    if (row < w.end && from[i] >= 0)   // (from the order 0 4, 1 5, 2 6, 3 7)
-      *reinterpret_cast<uint4*>(dst + row * a.stride) =
+    if (held >> i & 1u)   // (from the order 0 4, 1 5, 2 6, 3 7)
+      *reinterpret_cast<uint4*>(dst + i * step) =
           make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.x, v.y, 0x7632),
                      __byte_perm(v.z, v.w, 0x7632));
   }
