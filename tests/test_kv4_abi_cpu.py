@@ -31,7 +31,7 @@ def _handles(dp, cache=None, batch=None):
 @pytest.mark.parametrize("cache,batch,want", [
     (dict(head_dim=96), {}, 2), (dict(head_dim=256), {}, 2), (dict(head_dim=0), {}, 1), (dict(block_tokens=8), {}, 2),
     (dict(block_tokens=48), {}, 2), (dict(block_tokens=256), {}, 2), (dict(block_tokens=-16), {}, 1),
-    (dict(num_blocks=0), {}, 1), (dict(kv_heads=0), {}, 1), (dict(kv_heads=1024), {}, 2), (dict(k_codes=None), {}, 1),
+    (dict(num_blocks=1 << 27), {}, 2), (dict(num_blocks=0), {}, 1), (dict(kv_heads=0), {}, 1), (dict(kv_heads=1024), {}, 2), (dict(k_codes=None), {}, 1),
     (dict(v_codes=72), {}, 1), (dict(k_scales=None), {}, 1), (dict(k_scales=72), {}, 1), (dict(v_scales=66), {}, 1),
     ({}, dict(seqs=-1), 1), ({}, dict(seqs=65536), 2), ({}, dict(tokens=-1), 1), ({}, dict(max_tokens=-1), 1),
     ({}, dict(max_tokens=65536, tokens=70000), 2), ({}, dict(max_len=(1 << 27) + 1, table_stride=1 << 28), 2),

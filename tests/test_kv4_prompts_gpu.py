@@ -170,3 +170,65 @@ def test_the_largest_values_where_no_query_looks(dp, n, D):  # noqa: F811
             cache[kv][page, :, slots], cache[kv + 1][page, :, slots] = 0x88, 0x4612
     again, _ = _attend(dp, cache, q, cu, lens, table, window=50)
     assert np.array_equal(got, again)
+
+
+@pytest.mark.parametrize("ns,lens,g", [([64, 40], [0, 9000], 8), ([20, 40, 30], [7, 7000, 0], 4)])
+def test_padding_slots_beside_tasks_that_are_cut(dp, ns, lens, g):  # noqa: F811
+    """Rows of sequences of length zero, or longer than their sequence, see nothing in any part."""
+    rng = np.random.default_rng(g)
+    cu, lens, table, blocks = ref.random_batch(rng, ns, lens, 32)
+    _check(dp, ref.random_cache(rng, blocks, 2, 32, 128), _rows(rng, sum(ns), 2 * g, 128), cu, lens, table)
+
+
+def test_fewer_rows_than_declared(dp):  # noqa: F811
+    """A batch padded to its bounds: more tokens, rows and length declared than there are; the rest stays as it is."""
+    rng = np.random.default_rng(1)
+    for ns, lens, g in (([3, 1], [40, 900], 2), ([30, 90], [2000, 300], 4), ([560], [3000], 1)):
+        cu, lens, table, blocks = ref.random_batch(rng, ns, lens, 16)
+        table = np.pad(table, ((0, 0), (0, 100)), constant_values=-1)
+        cache = ref.random_cache(rng, blocks, 2, 16, 128)
+        T = sum(ns)
+        kc, vc, cut, lt, tt = _cuda(cache[0], cache[2], cu, lens, table)
+        ks, vs = (torch.from_numpy(b.astype(np.int32)).to(torch.int16).cuda().view(torch.bfloat16) for b in (cache[1], cache[3]))
+        c = dp.Kv4Cache(kc, vc, ks, vs)
+        b = dp.Kv8Batch(cut, lt, tt, tokens=T + 900, max_tokens=max(ns) + 700, max_len=int(lens.max()) + 1500)
+        q, out = _rows(rng, T + 900, 2 * g, 128), torch.full((T + 900, 2 * g, 128), 7.0, dtype=torch.float16, device="cuda")
+        dp.dptq_kv4_attention(c, b, q, out, 0.09)
+        want, tol = ref.attend(cache, q[:T].cpu().numpy(), cu, lens, table, 0.09)
+        assert (np.abs(out[:T].cpu().numpy() - want) <= tol).all() and (out[T:] == 7).all()
+        k, v = (torch.full((T + 900, 2, 128), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+        dp.dptq_kv4_read(c, b, k, v)
+        e = np.full((T + 900, 2, 128), 7, np.float16)
+        ref.read(cache[0], cache[1], e, cu, lens, table)
+        assert np.array_equal(k.cpu().numpy(), e)
+        x = q.clone()
+        dp.dptq_rotary(dp.Rotary(128), b, x)
+        assert torch.equal(x[T:], q[T:]) and not torch.equal(x[:T], q[:T])
+        new = _rows(rng, T + 900, 2, 128)
+        dp.dptq_kv4_append(c, b, new, new)
+        ref.append(cache[0], cache[1], new[:T].cpu().numpy(), cu, lens, table)
+        assert np.array_equal(c.k_codes.cpu().numpy(), cache[0])
+        dp.dptq_last_device_error()
+
+
+@pytest.mark.parametrize("H,D", [(1023, 64), (1000, 128)])
+def test_many_heads(dp, H, D):  # noqa: F811
+    rng = np.random.default_rng(H)
+    cu, lens, table, blocks = ref.random_batch(rng, [2, 1], [18, 5], 16)
+    cache = ref.random_cache(rng, blocks, H, 16, D)
+    q = _rows(rng, 3, H, D)
+    _check(dp, cache, q, cu, lens, table)
+    kc, vc, cut, lt, tt = _cuda(cache[0], cache[2], cu, lens, table)
+    ks, vs = (torch.from_numpy(b.astype(np.int32)).to(torch.int16).cuda().view(torch.bfloat16) for b in (cache[1], cache[3]))
+    c, b = dp.Kv4Cache(kc, vc, ks, vs), dp.Kv8Batch(cut, lt, tt, tokens=3, max_tokens=2, max_len=18)
+    k, v = _rows(rng, 3, H, D), _rows(rng, 3, H, D)
+    dp.dptq_kv4_append(c, b, k, v)
+    ref.append(cache[0], cache[1], k.cpu().numpy(), cu, lens, table)
+    ref.append(cache[2], cache[3], v.cpu().numpy(), cu, lens, table)
+    assert np.array_equal(c.k_codes.cpu().numpy(), cache[0]) and np.array_equal(c.v_codes.cpu().numpy(), cache[2])
+    back = [torch.empty_like(k) for _ in range(2)]
+    dp.dptq_kv4_read(c, b, *back)
+    e = np.zeros((3, H, D), np.float16)
+    ref.read(cache[2], cache[3], e, cu, lens, table)
+    assert np.array_equal(back[1].cpu().numpy(), e)
+    dp.dptq_last_device_error()
