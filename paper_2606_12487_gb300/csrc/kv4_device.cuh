@@ -85,12 +85,13 @@ struct Nibbles {
     return make_uint4(v[0], v[1], v[2], v[3]);
   }
 };
-// The values for any scale: each product in fp32, rounded once.  FINITE: at most the largest number of binary16.
+// The values for any scale: each product in fp32, rounded once.  FINITE: at most the largest number of binary16 (NaN stays:
+// it marks the K rows of keys whose scale is no number, and fmin and fmax would lose it).
 template <bool FINITE>
 __device__ __forceinline__ uint4 values_slow(uint32_t w, float s) {
   auto value = [&](int e) {
     const float v = s * (float)((int)(w << (28 - 4 * e)) >> 28);
-    return FINITE ? fminf(fmaxf(v, -65504.f), 65504.f) : v;
+    return FINITE && fabsf(v) > 65504.f ? copysignf(65504.f, v) : v;
   };
   return make_uint4(pack_half2(value(0), value(4)), pack_half2(value(1), value(5)), pack_half2(value(2), value(6)),
                     pack_half2(value(3), value(7)));
