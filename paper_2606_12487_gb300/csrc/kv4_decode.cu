@@ -18,8 +18,10 @@
 // stay in fp32, and the weights that go into the second product are p_j sv_j relative to 2^-15 of the largest of
 // them: binary16 holds 29 binades of those without loss.  The denominator takes each back by 1 / sv.
 //
-// K's codes enter as code + 8 times a power of two, which takes one instruction a pair to make, and a row's sum starts at
-// -8 times the sum of its q.  (V's do not: what cancels there is 8 times the sum of the weights, and outputs next to zero do not survive it.)
+// Both operands are the codes themselves.  (K's nibbles as code + 8, one instruction less a pair, a row's sum starting at -8 times the sum of
+// its q: errors go by 8 sum |q| then, which a channel of q far above the others, over keys with the code 0 there, brings into the
+// logits, for 121 instead of 122 us at the first size below, and 161 instead of 159 with two rows each of 64 sequences of 8000.  V's: what
+// cancels is 8 times the sum of the weights, and outputs next to zero do not survive it.)
 //
 // 64 ragged sequences up to 16384 tokens, 64 over 8 heads of 128 (590 MB): 120 us, 4.9 TB/s (its copies alone take 100 us, its
 // instructions alone 110); 32 up to 4096, 32 heads (298 MB): 71 us, of 64 53 us; one of 131072 tokens, 8 heads (138 MB): 40 us;
@@ -93,7 +95,7 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
   const uint8_t *k_from = A.k.codes[0] + 16 * lane, *v_from = A.k.codes[1] + 16 * lane;
   const uint8_t* s_from = reinterpret_cast<const uint8_t*>(lane / (2 * NG) ? A.k.scales[1] : A.k.scales[0]) + 16 * (lane & 1);
   const Nibbles nib;
-  const float unit = A.scale * (1.4426950408889634f * 0x1p24f);
+  const float unit = A.scale * 1.4426950408889634f;
 
   pdl_launch_dependents();
   pdl_wait();
@@ -102,8 +104,7 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
     const int rows = q.n * A.group;
     // ---- this share's rows of q, in the order of the dims that a widened word has
     uint32_t qf[RT][D / 16][2];
-    float off[RT][2];   // -8 2^-24 times the sum of q, of the two rows whose logits this lane holds
-    int pos[RT][2];     // their positions
+    int pos[RT][2];   // positions of the two rows whose logits this lane holds
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       // (lanes without a row read the first one: a load in a branch would wait for its own data)
@@ -118,21 +119,10 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         qf[r][2 * w + 1][0] = __byte_perm(v.x, v.z, 0x7632);
         qf[r][2 * w + 1][1] = __byte_perm(v.y, v.w, 0x7632);
       }
-      float sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&qf[r][k][e]));
-          sum += f.x + f.y;
-        }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);   // (of row g)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int mine = 8 * r + 2 * t + e;
         pos[r][e] = mine < rows ? q.start + mine / A.group : -1;
-        off[r][e] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, 4 * (2 * t + e));
       }
     }
     // weighted values of two rows, dims VB g + 2 j and the next
@@ -206,11 +196,10 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
       float x[NG][RT][4];
 #pragma unroll
       for (int h = 0; h < NG; ++h) {
-        float y[RT][4];
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[h][r][e] = off[r][e & 1], y[r][e] = 0.f;
+          for (int e = 0; e < 4; ++e) x[h][r][e] = 0.f;
         uint32_t w0[KW], w1[KW];
         const uint8_t* p0 = ck + k_lane + 8 * D * h;
         const uint8_t* p1 = p0 + 4 * D;
@@ -225,19 +214,15 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
         }
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
-          const uint32_t s0 = w0[w] >> 8, s1 = w1[w] >> 8;
+          __half2 a[4], b[4];
+          nib.codes(w0[w], a);
+          nib.codes(w1[w], b);
 #pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            mma_16816(x[h][r], nib.tiny<false>(w0[w]), nib.tiny<false>(w1[w]), nib.tiny<false>(s0), nib.tiny<false>(s1), qf[r][2 * w][0],
-                      qf[r][2 * w][1]);
-            mma_16816(y[r], nib.tiny<true>(w0[w]), nib.tiny<true>(w1[w]), nib.tiny<true>(s0), nib.tiny<true>(s1), qf[r][2 * w + 1][0],
-                      qf[r][2 * w + 1][1]);
-          }
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              mma_16816(x[h][r], bits(a[k]), bits(b[k]), bits(a[k + 2]), bits(b[k + 2]), qf[r][2 * w + k][0], qf[r][2 * w + k][1]);
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[h][r][e] = fmaf(y[r][e], 0x1p-4f, x[h][r][e]);
       }
       __syncwarp();
 #pragma unroll

@@ -41,24 +41,17 @@ __device__ __forceinline__ bool kv4_odd(uint32_t scale_bits) { return scale_bits
 // The nibbles of a word of eight codes, two a register, in the order 0 4, 1 5, 2 6, 3 7.  A nibble with its sign flipped is
 // code + 8.  With its constants in registers a mask and the flip are one instruction.
 struct Nibbles {
-  uint32_t lo, hi, wide_lo, wide_hi, tiny_lo, tiny_hi;
+  uint32_t lo, hi, wide_lo, wide_hi;
   __device__ __forceinline__ Nibbles() {
     asm("mov.b32 %0, 0x000F000F;" : "=r"(lo));
     asm("mov.b32 %0, 0x00F000F0;" : "=r"(hi));
     asm("mov.b32 %0, 0x64086408;" : "=r"(wide_lo));
     asm("mov.b32 %0, 0x64806480;" : "=r"(wide_hi));
-    asm("mov.b32 %0, 0x00080008;" : "=r"(tiny_lo));
-    asm("mov.b32 %0, 0x00800080;" : "=r"(tiny_hi));
   }
   static __device__ __forceinline__ uint32_t and_xor(uint32_t w, uint32_t mask, uint32_t flip) {
     uint32_t d;
     asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(d) : "r"(w), "r"(mask), "r"(flip));
     return d;
-  }
-  // Nibbles 0 and 4 (HI: 1 and 5), plus 8, as binary16 numbers below its normal range: (code + 8) 2^-24 (HI: 2^-20).
-  template <bool HI>
-  __device__ __forceinline__ uint32_t tiny(uint32_t w) const {
-    return HI ? and_xor(w, hi, tiny_hi) : and_xor(w, lo, tiny_lo);
   }
   // The codes as binary16: under the exponent of 1024 a nibble reads 1032 + code, four bits higher 1024 + 16 (code + 8); one
   // subtraction or fma, exact, takes the offset off.
