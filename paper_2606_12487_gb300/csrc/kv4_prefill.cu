@@ -727,7 +727,8 @@ static cudaError_t launch_prefill4(const Kv4AttendArgs& a, int num_sms, cudaStre
   // The tasks that would be cut are the last ones, with the fewest keys: those of a call's context, or, where all tasks run
   // at once, up to all of its keys.  A part has two tiles of 128 keys at least.
   const long long keys = keys_seen(a, tasks < P ? c.max_len : c.max_len - c.max_tokens);
-  if (c.seqs > kFewSeqs || tasks >= kCutWaves * P || 3 * (tasks % P) > 2 * P || keys < kCutKeys) {
+  // (P = 1: no task is ever left over)
+  if (P < 2 || c.seqs > kFewSeqs || tasks >= kCutWaves * P || 3 * (tasks % P) > 2 * P || keys < kCutKeys) {
     const auto fn = kv4_prefill_kernel<D, PAIR, false>;
     const cudaError_t e = ensure_max_dyn_smem(fn);
     if (e != cudaSuccess) return e;
