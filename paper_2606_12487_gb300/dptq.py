@@ -329,6 +329,14 @@ def dptq_add_rmsnorm_quant(x, residual, gamma, eps: float, bits: int, residual_o
                                          _ptr(codes), _ptr(scales), _stream(stream)))
 
 
+def _one_device(what, *tensors) -> int:
+    """The device of `tensors`, which have to be on one."""
+    device = tensors[0].get_device()
+    if any(t.get_device() != device for t in tensors[1:]):
+        raise ValueError(f"{what} must be on one device")
+    return device
+
+
 class Kv8Cache:
     """A paged KV cache of int8 codes: codes int8 [num_blocks, kv_heads, block_tokens, head_dim]
     and scales float32 [num_blocks, kv_heads], for K and for V.  Keeps the tensors."""
@@ -344,6 +352,7 @@ class Kv8Cache:
         _check_tensor(v_scales, torch.float32, (n, h), "v_scales")
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
         self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim = n, h, b, d
+        self.device = _one_device("a cache's tensors", k_codes, v_codes, k_scales, v_scales)
         self._c = _Kv8CacheC(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), n, h, b, d)
         self._ref = ctypes.addressof(self._c)
 
@@ -370,7 +379,7 @@ class Kv8Batch:
         _check_tensor(block_table, torch.int32, (S, block_table.shape[1]), "block_table")
         self.cu_tokens, self.seq_lens, self.block_table = cu_tokens, seq_lens, block_table
         self.tokens = tokens
-        self.device = seq_lens.get_device()
+        self.device = _one_device("a batch's arrays", seq_lens, cu_tokens, block_table)
         self._c = _Kv8BatchC(_ptr(cu_tokens), _ptr(seq_lens), _ptr(block_table), S, block_table.shape[1], tokens,
                              max_tokens, max_len)
         self._ref = ctypes.addressof(self._c)
@@ -421,7 +430,8 @@ def dptq_kv8_append(cache: Kv8Cache, batch: Kv8Batch, k, v, stream=None):
     s = _check_heads(k, batch.tokens, cache.kv_heads, cache.head_dim, "k")
     if s != _check_heads(v, batch.tokens, cache.kv_heads, cache.head_dim, "v"):
         raise ValueError("k and v must have the same distance between tokens")
-    _check(load().dptq_kv8_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, _stream(stream)))
+    at = _launch_stream(stream, cache.device, batch.device, k.get_device(), v.get_device())
+    _check(load().dptq_kv8_append(cache._ref, batch._ref, k.data_ptr(), v.data_ptr(), s, at))
 
 
 def dptq_kv8_attention(cache: Kv8Cache, batch: Kv8Batch, q, out, scale: float, window: int = 0, sinks: int = 0,
@@ -432,8 +442,9 @@ def dptq_kv8_attention(cache: Kv8Cache, batch: Kv8Batch, q, out, scale: float, w
     H = q.shape[1]
     qs = _check_heads(q, batch.tokens, H, cache.head_dim, "q")
     os_ = _check_heads(out, batch.tokens, H, cache.head_dim, "out")
+    at = _launch_stream(stream, cache.device, batch.device, q.get_device(), out.get_device())
     _check(load().dptq_kv8_attention(cache._ref, batch._ref, q.data_ptr(), qs, H, scale, window, sinks,
-                                     out.data_ptr(), os_, _stream(stream)))
+                                     out.data_ptr(), os_, at))
 
 
 class Kv4Cache:
@@ -453,9 +464,7 @@ class Kv4Cache:
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
         load()
         self.num_blocks, self.kv_heads, self.block_tokens, self.head_dim = n, h, b, 2 * d
-        self.device = k_codes.get_device()
-        if any(t.get_device() != self.device for t in (v_codes, k_scales, v_scales)):
-            raise ValueError("a cache's tensors must be on one device")
+        self.device = _one_device("a cache's tensors", k_codes, v_codes, k_scales, v_scales)
         self._c = _Kv4CacheC(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), n, h, b, 2 * d)
         self._ref = ctypes.addressof(self._c)
 
