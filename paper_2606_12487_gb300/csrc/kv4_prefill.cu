@@ -36,6 +36,14 @@
 namespace dptq {
 
 constexpr float kUnit = 7.f;   // weights are relative to 2^-7 of the largest
+// Rows whose largest score is more than that, in powers of two, are made from S - m, apart from the others: log2(e) scale S + (7 - m) in
+// one fma is off by a step of m, 2^-10 here and 2 at 2^25, where weights would be too large whatever m is.  (All rows that
+// way: 849 instead of 827 us for a prompt of 8192 tokens, 64 over 8 heads.)
+constexpr float kFar = 16384.f;
+// log2(e) |scale|, above 0 so that a masked score of -inf stays, and finite so that the largest score's difference to itself is 0.
+__device__ __forceinline__ float kv4_unit(float scale) {
+  return fminf(fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f), 1e37f);
+}
 
 // Where the rows of a CTA or pair go: slot of the scratch for a part of a task's keys, -1 for whole tasks.
 struct Out {
@@ -240,9 +248,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
     const int pos = mine ? q.start + row / A.group : -1;
     const uint32_t tlane = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tm + tlane + t * 128, tO = tm + tlane + 256 + t * 128;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, far_m = 0.f, l = 0.f;   // the largest score so far: m, or far_m where that is not 0 (m is then -inf)
     bool ok = true;
-    const float unit = fmaxf(fabsf(A.scale) * 1.4426950408889634f, 1e-37f);   // (above 0: a masked -inf stays)
+    const float unit = kv4_unit(A.scale);
     if (t < halves && nt > 0) {
       {   // the warp's rows of q, whole rows at a time, in the order of the dims that a widened word has, negated for a
           // negative scale
@@ -290,7 +298,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
         uint32_t p[32];
         // A quarter's weights, packed, and their sum.
         auto quarter = [&](float (&x)[32], uint32_t* w, float& s) {
-          const float off = kUnit - (m == -INFINITY ? 0.f : m);
+          const float off = fmaf(m == -INFINITY ? 0.f : -m, unit, kUnit);
           const uint64_t a = f2_pack(unit, unit), b = f2_pack(off, off);
           uint64_t sum = 0;
 #pragma unroll
@@ -313,6 +321,15 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
           v[10] = fmaxf(x[30], x[31]);
           return fmaxf(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[8])), fmaxf(v[9], v[10]));
         };
+        auto far = [&](float v) { return fabsf(v) * unit > kFar && fabsf(v) < INFINITY; };
+        // A half's weights are stored, and the next half's scores asked for.
+        auto give = [&](int n) {
+          tmem_st32(tS + 64 + 32 * n, p);
+          if (n == 0) tmem_ld32(tS, xa);
+          tmem_st_wait();
+          tc_fence_before();
+          tell_first(&S.pfull[t][n], false);
+        };
         if (j == 0) {   // the first maximum, so that the first half is not made for nothing
 #pragma unroll 1
           for (int h = 0; h < 4; ++h) {
@@ -321,8 +338,9 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
             float v = xa[0];
 #pragma unroll
             for (int k = 1; k < 31; k += 2) v = max3(v, xa[k], xa[k + 1]);
-            m = fmaxf(m, unit * fmaxf(v, xa[31]));
+            m = fmaxf(m, fmaxf(v, xa[31]));
           }
+          if (far(m)) m = -INFINITY;
         }
         tmem_ld32(tS + 64, xa);
         int n = 0;
@@ -340,24 +358,25 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
             quarter(xa, p, s);
             tmem_ld_arrived(xb);
             quarter(xb, p + 16, s);
-            // The sum says whether a weight may be above 2^15: the scores' maximum is looked for only then, and where no
-            // key has been seen yet.
+            // The sum says whether a weight may be above 2^15: the scores' maximum is looked for only then, and where there is
+            // no m.  (A sum above 2^15 has a weight above 2^8, so a score is above m; relative to the half's own maximum no
+            // weight is above 2^7 but for the rounding that kFar bounds, and 64 of them make no such sum: a half is made
+            // again once.)
             if (__any_sync(0xffffffffu, s > 32768.f || m == -INFINITY)) {
-              top = unit * fmaxf(largest(xa), largest(xb));
+              top = fmaxf(largest(xa), largest(xb));
               more = s > 32768.f || (m == -INFINITY && top > m);
               if (__any_sync(0xffffffffu, more)) break;
             }
             l += s;
-            tmem_st32(tS + 64 + 32 * n, p);
-            if (n == 0) tmem_ld32(tS, xa);
-            tmem_st_wait();
-            tc_fence_before();
-            tell_first(&S.pfull[t][n], false);
+            give(n);
           }
           if (n == 2) break;
           // (a row whose own maximum may still lag keeps it: its result has nothing to do with the warp's other rows)
-          const float mn = more ? top : m, f = mn == m ? 1.f : exp2_fast(m - mn);   // (m = -inf: no key yet)
-          m = mn;
+          const float was = far_m != 0.f ? far_m : m;   // (-inf: no key yet)
+          const float now = far_m != 0.f ? fmaxf(far_m, top) : more ? top : m;
+          const float f = now == was ? 1.f : exp2_fast((was - now) * unit);
+          m = far(now) ? -INFINITY : now;
+          far_m = far(now) ? now : 0.f;
           l *= f;
           // O: PV of tile j - 1 came before S of tile j, which is here; of tile j, the first half's
           // product may be under way.
@@ -377,7 +396,19 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
               tmem_st16(tO + k, o);
             }
           }
-          tmem_ld32(tS + 64 * (1 - n), xa);
+          if (!__any_sync(0xffffffffu, far_m != 0.f)) {
+            tmem_ld32(tS + 64 * (1 - n), xa);
+            continue;
+          }
+          // A warp with such rows makes its half here (x - 0 for the others: the weights and sums that they have anyway).
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) xa[k] -= far_m, xb[k] -= far_m;
+          quarter(xa, p, s);
+          quarter(xb, p + 16, s);
+          l += s;
+          give(n);
+          if (++n == 2) break;
         }
       }
       if (ok) ok = wait_one(&S.ofull[t], 0, abort_flag, c.err, kDevTimeoutTmemFull, A.wait_cycles);
@@ -397,7 +428,7 @@ __global__ void __launch_bounds__(kPreThreads, 1) kv4_prefill_kernel(const Kv4At
       if (sums_only) {   // weighted values [kRows][D], then maxima, then sums
         sums = A.ws + (size_t)w.slot * (kRows * (D + 2));
         if (mine) {
-          sums[kRows * D + at] = m;
+          sums[kRows * D + at] = far_m != 0.f ? far_m : m;
           sums[kRows * (D + 1) + at] = l;
         }
         sums += (size_t)at * D;
@@ -681,7 +712,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(const Kv4AttendA
   for (int k = lane; k < cut.parts; k += 32) M = fmaxf(M, __ldcg(sums + k * pitch + (size_t)rows * D + r));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  const float base = M == -INFINITY ? 0.f : M;
+  const float base = M == -INFINITY ? 0.f : M, unit = kv4_unit(A.scale);
   constexpr int E = D / 32;
   float l = 0.f, o[E];
 #pragma unroll
@@ -689,7 +720,7 @@ __global__ void __launch_bounds__(kJoinThreads) kv4_join_kernel(const Kv4AttendA
 #pragma unroll 4
   for (int k = 0; k < cut.parts; ++k) {
     const float* p = sums + k * pitch;
-    const float f = exp2_fast(__ldcg(p + (size_t)rows * D + r) - base);
+    const float f = exp2_fast((__ldcg(p + (size_t)rows * D + r) - base) * unit);
     l = fmaf(f, __ldcg(p + (size_t)rows * (D + 1) + r), l);
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = fmaf(f, __ldcg(p + (size_t)r * D + E * lane + e), o[e]);
