@@ -278,7 +278,8 @@ kv4_decode_kernel(const Kv4AttendArgs A) {
       uint32_t pf[NG][RT][2];   // B fragments of the weights, per 16 keys
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const float m0 = m[r][0] == -INFINITY ? 0.f : m[r][0] - kDecUnit, m1 = m[r][1] == -INFINITY ? 0.f : m[r][1] - kDecUnit;
+        // (rounded up: a weight above 2^15 may be none that binary16 holds)
+        const float m0 = m[r][0] == -INFINITY ? 0.f : __fsub_ru(m[r][0], kDecUnit), m1 = m[r][1] == -INFINITY ? 0.f : __fsub_ru(m[r][1], kDecUnit);
 #pragma unroll
         for (int h = 0; h < NG; ++h) {
           const float p0 = exp2_fast(x[h][r][0] - m0), p1 = exp2_fast(x[h][r][1] - m1);

@@ -11,8 +11,8 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 LARGEST = 0x4612     # 9344
-# alone, heads of 64; alone; cut along the keys; pairs; pairs cut along the keys
-FORMS = [([300], [900], 8, 2, 64),
+# few rows, one and two row tiles; prompts: alone, heads of 64; alone; cut along the keys; pairs; pairs cut along the keys
+FORMS = [([1], [90], 2, 1, 64), ([1, 1], [2000, 700], 2, 8, 128), ([4], [700], 2, 4, 128), ([300], [900], 8, 2, 64),
          ([130] * 20, [500] * 20, 8, 1, 128), ([200], [3000], 2, 1, 128), ([600], [2700], 20, 2, 128), ([600], [3500], 2, 1, 128)]
 
 
