@@ -61,11 +61,6 @@ __device__ __forceinline__ float log2_fast(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // Keys of a step, in 16s.  Four, with three CTAs an SM, 64 ragged sequences: 120 us; two: 138, with four CTAs an SM 143.  Two rows of each
 // of 64 sequences of 8000: 161 / 178 us.
 constexpr int kNG = 4;

@@ -76,11 +76,6 @@ __device__ __forceinline__ void tmem_ld_arrived(float (&r)[32]) {
                  "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]),
                  "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])::"memory");
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 template <int N>
 __device__ __forceinline__ void reg_more() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -115,9 +110,8 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
 }
 
 // Writes -inf over the scores of the keys that this thread's row does not see (gone: bit g, of the tile's keys 16 g ..,
-// none does), in tensor memory: the
-// few tiles that need it pay for the pass, and the code that every tile runs stays short (with
-// the masks in its middle, 929 instead of 855 us for a prompt of 8192 tokens, 64 over 8 heads).
+// none does), in tensor memory: the few tiles that need it pay for the pass, and the code that every tile runs stays short
+// (with the masks in its middle, 929 instead of 855 us for a prompt of 8192 tokens, 64 over 8 heads, int8 cache).
 __device__ __forceinline__ void mask_scores(uint32_t tS, int pos, int key, int window, int sinks,
                                             uint32_t gone = 0) {
 #pragma unroll 1
@@ -126,7 +120,6 @@ __device__ __forceinline__ void mask_scores(uint32_t tS, int pos, int key, int w
     tmem_ld16(tS + k, v);
     uint32_t bits = low_bits(pos - key - k + 1);   // bit e: the row sees key k + e
     if (window > 0) bits &= ~low_bits(pos - window + 1 - key - k) | low_bits(sinks - key - k);
-    if (gone >> (k / 16) & 1u) bits = 0;
     if (gone >> (k / 16) & 1u) bits = 0;
     tmem_ld_wait();
 #pragma unroll
