@@ -248,7 +248,8 @@ dptq_status dptq_kv8_append(const dptq_kv8_cache* cache, const dptq_kv8_batch* b
  * lost by it), and NaN in q stays in its row.
  * The integer codes enter the tensor cores exactly (int8 fits in binary16), the scales are
  * applied in fp32; softmax weights times V scale are rounded to binary16 relative to their
- * largest so far; logits, maxima, sums and accumulators are fp32.
+ * largest so far; logits, maxima, sums and accumulators are fp32.  Calls of more than 16 rows for a sequence and KV head
+ * take logits up to 2^25 in size; rows with larger ones are unspecified.
  * q_fp16, out_fp16: device rows of `tokens` tokens, q_heads * head_dim binary16 values each, rows
  * q_stride / out_stride elements apart; 16-byte aligned, strides multiples of 8.
  * q_heads a multiple of kv_heads, at most 64 times as many.  window, sinks >= 0.
@@ -262,8 +263,10 @@ dptq_status dptq_kv8_attention(const dptq_kv8_cache* cache, const dptq_kv8_batch
  * device, so that none of them allocates (for example before a stream capture).  Synchronous. */
 dptq_status dptq_kv8_reserve(void);
 
-/* ---- Rotary positions, and the 4-bit KV cache (Section 4.2, Algorithm 1 steps 1 and 4: symmetric, groups
- * along the head dimension, here one group a token and head) with its attention.  The batch is the one above. */
+/* ---- Rotary positions, and the 4-bit KV cache with its attention.  (The paper keeps the KV cache in 4 bits, in groups of
+ * 128 values (Section 4.2, Algorithm 1 steps 1 and 4), and leaves the quantizer's form, the cache's layout and the kernels
+ * open.  Here a group is a token's values of one KV head, 128 or 64 of them, and the quantizer is symmetric.)  The batch
+ * is the one above. */
 
 /* A paged KV cache of 4-bit codes with one scale for each token and KV head.  Codes uint8
  * [num_blocks][kv_heads][block_tokens][head_dim / 2] in the nibble format of
@@ -271,8 +274,8 @@ dptq_status dptq_kv8_reserve(void);
  * [num_blocks][kv_heads][block_tokens].  Codes and scales 16-byte aligned.  A cached value is
  * binary16(scale * code), which is exact for scales of 2^-17 and more (8 + 3 significant bits): the tensor
  * cores, the read-back and the definition below all see the same values.  Scales are 0 to 9344, the largest that
- * dptq_kv4_append makes of finite values; anything else counts as no number in dptq_kv4_attention.  Codes are -7 to 7; what
- * is stored at positions that no query sees is of no consequence.  head_dim 64 or 128;
+ * dptq_kv4_append makes of finite values; anything else, -0 too, counts as no number in dptq_kv4_attention.  Codes
+ * are -7 to 7; what is stored at positions that no query sees is of no consequence.  head_dim 64 or 128;
  * block_tokens 16, 32, 64 or 128; num_blocks * kv_heads * block_tokens below 2^32 (UNSUPPORTED otherwise).
  * All device memory of the caller; the struct is read during the call only. */
 typedef struct dptq_kv4_cache {
@@ -286,8 +289,10 @@ typedef struct dptq_kv4_cache {
 /* Quantize the K and V rows of new tokens into the cache, each token and head on its own:
  *   scale = bfloat16(max|x| * fl(1 / 7)), rounded to nearest even;  code = round-half-even(x / scale), the IEEE
  *   fp32 quotient;  scale 0 gives codes 0.
- * Codes are in [-7, 7].  A NaN counts for nothing in the maximum and takes the code 0; a row with an
- * infinite value has an infinite scale and codes 0.  Earlier tokens of a page are not touched.
+ * Codes are in [-7, 7].  A value is kept within half a scale, (1 + 2^-8) max|x| / 14: codes may differ from
+ * dptq_kv4_quantize's, whose scale is not rounded to bfloat16, its bound is 2^-8 of it smaller.  A NaN counts for nothing
+ * in the maximum and takes the code 0; a row with an infinite value has an infinite scale and codes 0.  Earlier tokens of a
+ * page are not touched.
  * A position is written by one row of the batch at most.  Arguments, rows and errors as dptq_kv8_append. */
 dptq_status dptq_kv4_append(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* k_fp16,
                             const void* v_fp16, long long token_stride, void* stream);
@@ -295,8 +300,8 @@ dptq_status dptq_kv4_append(const dptq_kv4_cache* cache, const dptq_kv8_batch* b
 /* The cached values of the batch's rows, binary16(scale * code): row i of a sequence's n gets the K and V
  * heads of position seq_lens - n + i (rows of the whole sequence: cu_tokens with n = seq_lens).
  * k_out, v_out: device rows of `tokens` tokens, kv_heads * head_dim binary16 values each, token_stride
- * elements apart; 16-byte aligned, token_stride a multiple of 8.  Rows at negative positions, and rows whose
- * page is out of range (INVALID_ARG from dptq_last_device_error), are left as they are.  A scale that is
+ * elements apart; 16-byte aligned, token_stride a multiple of 8; the two may not overlap.  Rows at negative
+ * positions, and rows whose page is out of range (INVALID_ARG from dptq_last_device_error), are left as they are.  A scale that is
  * infinite or NaN gives infinities and NaN as the product has them.  Errors as dptq_kv8_append. */
 dptq_status dptq_kv4_read(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, void* k_out, void* v_out,
                           long long token_stride, void* stream);
@@ -305,9 +310,11 @@ dptq_status dptq_kv4_read(const dptq_kv4_cache* cache, const dptq_kv8_batch* bat
  * h / (q_heads / kv_heads):
  *   out = sum_j softmax(scale * q . k_j)_j v_j  over the keys j that the query sees,
  * as dptq_kv8_attention defines them (window, sinks, zeros for a query that sees none).  A query that sees a key
- * whose K or V scale is no number (negative, above 9344, infinite or NaN) gets NaN; no other query is touched by it, and
- * NaN in q stays in its row.  Logits, maxima, sums and accumulators are fp32; softmax weights are rounded to binary16
- * relative to their largest so far.  Calls of at most 16 rows for each sequence and KV head take scale * code unrounded
+ * whose K or V scale is no number (the sign set, above 9344, infinite or NaN) gets NaN; no other query is touched by it,
+ * and NaN in q stays in its row.  Logits, maxima, sums and accumulators are fp32; the products in a logit are exact, so that
+ * its error goes by the sum of |q k|.  Softmax weights are rounded to binary16 relative to their largest so far (2^-11 of each;
+ * the sums that outputs are divided by are of the unrounded ones).  Finite inputs give finite outputs as long as fp32 holds
+ * the logits.  Calls of at most 16 rows for each sequence and KV head take scale * code unrounded
  * (scales below 2^-17: up to 2^-25 from the value above).
  * Uses the scratch of dptq_kv8_attention (dptq_kv8_reserve allocates it).  Arguments and errors as there. */
 dptq_status dptq_kv4_attention(const dptq_kv4_cache* cache, const dptq_kv8_batch* batch, const void* q_fp16,

@@ -151,7 +151,7 @@ struct Kv8AttendArgs {
 };
 // Most rows of a (sequence, KV head) in the decode kernel: 16 rows of 64 sequences, 8 KV heads, take 210 us there
 // and 462 us in the prompt kernel, whose row tiles are 128 rows, at 8000 tokens, 61 and 93 us at 500 to 2000; over the 4-bit
-// cache 161 and 433, 57 and 88 us.
+// cache 159 and 409, 53 and 85 us.
 constexpr int kDecodeRows = 16;
 // Decode grids: CTAs an SM for up to 8 and up to 16 rows; each CTA leaves partial results of two
 // (sequence, head)s at most: weighted values, maximum and sum of each row.

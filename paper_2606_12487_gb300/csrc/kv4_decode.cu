@@ -2,7 +2,7 @@
 // paged 4-bit cache: decode steps and a few speculative tokens.
 //
 // The call is a stream over the visible codes and scales (a byte for two values, read once), so bytes bound it, and
-// almost as closely the codes' way into the tensor cores: a step of 64 keys is about 1000 instructions of a warp.  Work is cut into equal
+// almost as closely the codes' way into the tensor cores: a step of 64 keys is about 1100 instructions of a warp.  Work is cut into equal
 // shares of steps (kv_decode.cuh); inside a CTA the warps take every fourth step, each with a ring of steps of its
 // own in shared memory, filled by asynchronous 16-byte copies (no barrier between warps).
 //
@@ -16,15 +16,17 @@
 //
 // Softmax in base 2 on x_j = log2(e) scale sk (q . ck_j) + log2(sv): codes are the exact operands, scales
 // stay in fp32, and the weights that go into the second product are p_j sv_j relative to 2^-15 of the largest of
-// them: binary16 holds 29 binades of those without loss.  The denominator takes each back by 1 / sv.
+// them: binary16 holds 29 binades of those at full precision.  They are rounded to it, 2^-11 of each (both operands of an MMA
+// have one type); the denominator, in fp32, takes each unrounded one back by 1 / sv.  The rms error of outputs is 2.21e-4 of
+// them instead of the 2.08e-4 of rounding the exact ones.
 //
 // Both operands are the codes themselves.  (K's nibbles as code + 8, one instruction less a pair, a row's sum starting at -8 times the sum of
 // its q: errors go by 8 sum |q| then, which a channel of q far above the others, over keys with the code 0 there, brings into the
 // logits, for 121 instead of 122 us at the first size below, and 161 instead of 159 with two rows each of 64 sequences of 8000.  V's: what
 // cancels is 8 times the sum of the weights, and outputs next to zero do not survive it.)
 //
-// 64 ragged sequences up to 16384 tokens, 64 over 8 heads of 128 (590 MB): 120 us, 4.9 TB/s (its copies alone take 100 us, its
-// instructions alone 110); 32 up to 4096, 32 heads (298 MB): 71 us, of 64 53 us; one of 131072 tokens, 8 heads (138 MB): 40 us;
+// 64 ragged sequences up to 16384 tokens, 64 over 8 heads of 128 (590 MB): 122.5 us, 4.8 TB/s (its copies alone take 98 us, its
+// instructions alone 113); 32 up to 4096, 32 heads (298 MB): 72 us, of 64 51 us; one of 131072 tokens, 8 heads (138 MB): 41 us;
 // one of 512: 9 us.
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -61,11 +63,11 @@ __device__ __forceinline__ float log2_fast(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Keys of a step, in 16s.  Four, with three CTAs an SM, 64 ragged sequences: 120 us; two: 138, with four CTAs an SM 143.  Two rows of each
-// of 64 sequences of 8000: 161 / 178 us.
+// Keys of a step, in 16s.  Four, with three CTAs an SM, 64 ragged sequences: 122 us; two: 139, and with four CTAs of shorter rings an
+// SM 139.  Two rows of each of 64 sequences of 8000, four / two: 159 / 178 us.
 constexpr int kNG = 4;
-// A power of two, a step a warp; and results of as many CTAs are joined at once: four sequences of 4000 tokens, 8 heads, 15.2 us (shares
-// without regard to heads, of 12 at once: 24.7), one of 8192 15.2 (19.7), one of 2048 12.0 (12.0), 16 up to 8000 over 4 heads 27.4 (29.7).
+// A power of two, a step a warp; and results of as many CTAs are joined at once: four sequences of 4000 tokens, 8 heads, 15.1 us (shares
+// without regard to heads, of 12 at once: 23.9), one of 8192 15.3 (19.0), one of 2048 11.7 (11.3), 16 up to 8000 over 4 heads 26.5 (29.4).
 constexpr int kDec4MinSteps = 4, kDec4Join = 20;
 constexpr float kDecUnit = 15.f;   // weights are relative to 2^-15 of the largest
 

@@ -7,9 +7,11 @@
 //   S = q k^T   128 x 128 x D   both operands in shared memory, S in tensor memory
 //   O += P v    128 x D x 128   P in tensor memory (over half of S), v in shared memory
 // A bfloat16 scale times a code is a binary16 number, so tiles are widened to the cached values themselves and the
-// softmax knows nothing of scales: x = log2(e) scale S, weights 2^(x - m + 7) relative to the row's maximum m, which
+// softmax knows nothing of scales: weights 2^(log2(e) scale (S - m) + 7) relative to the row's maximum m, which
 // may lag by 2^8 (O is rescaled only where it has grown by more): binary16 holds 2^15, and 21 binades
-// below the largest weight without loss.
+// below the largest weight at full precision.  The weights are rounded to it, 2^-11 of each, since both operands of an MMA have
+// V's type (fp32 ones would take tf32 MMAs, at half the rate, and twice P's room); sums are of the unrounded ones.  The rms error
+// of outputs is 2.23e-4 of them instead of the 2.08e-4 of rounding the exact ones.
 //
 // Warp roles: 0-3 and 4-7 softmax and output of the row tiles, a row a thread; 8-11 widen K and
 // V tiles (global to registers a tile ahead, then to shared memory in the 128-byte swizzle);
@@ -18,10 +20,10 @@
 // A task is the 256 rows (512 of a pair) of one (sequence, KV head).  Tasks that would leave SMs without work in the
 // last wave are split along the keys (Cut): each CTA leaves its rows' sums, and a second launch joins them.
 //
-// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 834 us, 1318 TFLOP/s, 68 % of the measured bf16 rate):
-// the chain of a row tile from S over its softmax back to the next S, in which widening and softmax share the issue slots: with the
-// softmax's work left out 735 us, with both left out 691 (all barriers kept), with the exponentials alone left out still 848 of the
-// 846 that it took then.  512 rows behind 16000 tokens: 220 us; three chunks up to 500 behind up to 12000, window 4096: 182 us.
+// What bounds it, at a prompt of 8192 tokens, 64 over 8 heads of 128 (1.1 TFLOP, 836 us, 1315 TFLOP/s, 68 % of the measured bf16 rate):
+// the chain of a row tile from S over its softmax back to the next S, in which widening and softmax share the issue slots: of the
+// 846 us of an earlier form, 735 were left without the softmax's work, 691 without both (all barriers kept), 848 without the
+// exponentials alone.  512 rows behind 16000 tokens: 220 us; three chunks up to 500 behind up to 12000, window 4096: 182 us.
 //
 // The order of the dims: a word of eight nibbles widens to the pairs (0, 4), (1, 5), (2, 6), (3, 7).  q is stored in
 // that order too, and the output's registers are written from it.
@@ -737,14 +739,14 @@ static long long keys_seen(const Kv4AttendArgs& a, long long keys) {
   return a.window > 0 ? std::min(keys, (long long)a.window + a.sinks + a.k.c.max_tokens) : keys;
 }
 // Pairs of CTAs take sequences of so many rows (of a KV head) and, on average over the rows, so many keys.  Pairs / CTAs
-// alone, us, 64 over 8 heads: 1 x 8192 838 / 942; 1 x 512 behind 16000 220 / 259; 1 x 2048 behind 8000 466 / 506; 16 x 100 behind
-// 4000 209 / 208; 1 x 1000 behind 100000 2555 / 3056; with fewer keys 32 heads, 8 x 512 64 / 47; 32 over 8, 3 x 2048 101 / 100.
+// alone, us, 64 over 8 heads: 1 x 8192 836 / 876; 1 x 512 behind 16000 220 / 240; 1 x 2048 behind 8000 463 / 483; 16 x 100 behind
+// 4000 213 / 191 (another wave); 1 x 1000 behind 100000 2558 / 2757; with fewer keys 32 heads, 8 x 512 64 / 46; 32 over 8, 3 x 2048 100 / 95.
 constexpr int kPairRows = 512, kPairKeys = 2048;
 // Calls of so many waves are not cut, since their tasks do not end together, and calls whose last tasks have fewer keys are
 // not, since the join costs more than it saves.
-// Cut / whole, us, 64 over 8 heads: 3 x 500 with a window of 4096 182 / 202; 16 x 100 behind 4000 209 / 226; 2048 behind 8000
-// 460 / 495 (3.4 waves each); 2 x 3000 behind up to 9000, 32 over 4 (4.2 waves) 599 / 581; 300 behind 300, 40 heads, 44 / 20; 3 x 2048 without a
-// context, 32 over 8, 140 / 100.
+// Cut / whole, us, 64 over 8 heads: 3 x 500 with a window of 4096 182 / 203; 16 x 100 behind 4000 213 / 229; 2048 behind 8000
+// 463 / 485 (3.4 waves each); 2 x 3000 behind up to 9000, 32 over 4 (4.2 waves) 595 / 582; 300 behind 300, 40 heads, 44 / 20; 4 x 1683
+// behind up to 873, 8 heads of 64, 50 / 38.
 constexpr int kCutWaves = 4, kCutKeys = 20 * kTileKeys;
 
 template <int D, bool PAIR>

@@ -10,7 +10,7 @@
 // Two bytes in, two out a value: bytes bound it.  The angles of a row serve all of its heads, so a CTA makes
 // them once in shared memory; a thread then keeps the eight of its place in a head and goes over the heads with
 // 16-byte loads and stores.  8192 rows of 72 heads of 128 (302 MB): 46.1 us in a graph, 6.5 TB/s; 1333 rows of 80, half of each head
-// turned, the other half copied: 12.1 us, 4.5 TB/s; one row of 40: 2.3 us.
+// turned, the other half copied: 12.1 us, 4.5 TB/s; one row of 40: 2.3 us (2.7 from HBM).
 #include <cstdint>
 #include <cuda_runtime.h>
 #include <cuda_fp16.h>
