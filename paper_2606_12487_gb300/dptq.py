@@ -367,7 +367,8 @@ class Kv8Cache:
 
 class Kv8Batch:
     """The sequences of one step: cu_tokens int32 [seqs + 1], seq_lens int32 [seqs] (cached
-    tokens with the step's own), block_table int32 [seqs, columns], all on the GPU; the host's
+    tokens with the step's own), block_table int32 [seqs, columns], all on one GPU (the current one
+    in the calls that take it, as every other tensor of theirs); the host's
     bounds `tokens` (cu_tokens[seqs]), `max_tokens` (of a sequence in this step) and `max_len`
     (of a sequence's length).  Keeps the tensors."""
 
